@@ -202,6 +202,108 @@ pot_status pot_store_values_int8(const uint16_t* v_fp16, int64_t n_seq, int64_t 
                                  int64_t t_cap, int64_t t0, uint8_t* v_u8,
                                  int8_t* v_exp, void* stream);
 
+/* Store fp16 values in 4 bits with a step and a minimum per token: 36 bytes per
+ * token instead of 128. Per token row v (d values): z = min v, s = the smallest
+ * fp16 number >= fl(fl(max v - min v) / 15) (fl: rounded to fp32), n =
+ * min(15, round-half-even(fl(fl(v - z) fl(1/s)))) (0 where s = 0), and the value
+ * is z + s n, within s/2 (1 + 2^-20) of v. Infinities count as +-65504; NaN elements
+ * are passed over by the minimum and the maximum and take n = 0 (a row of NaNs:
+ * z = s = 0), so a cache holds finite numbers only.
+ *  v_fp16   [n_seq][n_tok][d] fp16, dense, device (token-major rows).
+ *  v_u4     [B*Hkv][t_cap/8][POT_INT4_GROUP_BYTES] bytes, one record per 8
+ *           tokens: byte 16 (c % 16) + 8 (c / 32) + t % 8 holds n of dimension
+ *           c of token t, in its low half where c % 32 < 16 and in its high half
+ *           elsewhere (so a token shares no byte with another); from byte 256 the
+ *           8 tokens' s and from byte 272 their z, fp16.
+ * n_seq, n_tok, t_cap, t0 and the errors as pot_store_values; n_seq * n_tok up to
+ * 2^31. */
+#define POT_INT4_GROUP_BYTES 288
+pot_status pot_store_values_int4(const uint16_t* v_fp16, int64_t n_seq, int64_t n_tok,
+                                 int64_t t_cap, int64_t t0, uint8_t* v_u4, void* stream);
+
+/* Read a cache back: rows t0 .. t0+n_tok-1 of n_seq sequences (consecutive from
+ * the given pointers, t_cap rows each) as the dense fp16 rows that the codes stand
+ * for, [n_seq][n_tok][d]: for attention over a prompt, for checks, or to write them
+ * in another format. Nothing of the cache is changed, and rows outside the range are
+ * not read.
+ *  pot_load_keys: s sigma (1 + j/2^k) 2^-e of each element, 0 for the zero code,
+ *   formed in fp32 and rounded to fp16; with fmt->hadamard rotated back (H K^ / 8,
+ *   sums in fp32, rounded once). A format with hadamard = 0 gives the rows of a
+ *   rotated cache as they were encoded. codes_m NULL iff k = 0.
+ *  pot_load_values: the fp16 values as stored.
+ *  pot_load_values_int8: v^ 2^-g.
+ *  pot_load_values_int4: z + s n, formed in fp32 and rounded to fp16.
+ * t_cap a positive multiple of 8; sizes of 0 are no-ops. Errors as the store calls;
+ * n_seq * n_tok up to 2^31. */
+pot_status pot_load_keys(const pot_format* fmt, const uint8_t* codes_se, const uint8_t* codes_m,
+                         const float* key_scale, int64_t n_seq, int64_t n_tok, int64_t t_cap,
+                         int64_t t0, uint16_t* k_fp16, void* stream);
+pot_status pot_load_values(const uint16_t* v_cache, int64_t n_seq, int64_t n_tok, int64_t t_cap,
+                           int64_t t0, uint16_t* v_fp16, void* stream);
+pot_status pot_load_values_int8(const uint8_t* v_u8, const int8_t* v_exp, int64_t n_seq,
+                                int64_t n_tok, int64_t t_cap, int64_t t0, uint16_t* v_fp16,
+                                void* stream);
+pot_status pot_load_values_int4(const uint8_t* v_u4, int64_t n_seq, int64_t n_tok, int64_t t_cap,
+                                int64_t t0, uint16_t* v_fp16, void* stream);
+
+/* Types of a projection's rows. */
+typedef enum pot_dtype { POT_FP16 = 0, POT_BF16 = 1, POT_FP32 = 2 } pot_dtype;
+
+/* Position rotation of a head (rotary embedding).
+ *  head_dim     : 64.
+ *  rot_dim      : the first rot_dim elements of a head are rotated, the others pass
+ *                 (even, 0 .. 64; 0: no rotation).
+ *  neighbours   : pair i is elements (i, i + rot_dim/2) if 0, (2i, 2i + 1) if 1.
+ *  n_axes       : position axes, 1 .. POT_MAX_AXES (text 1; time, height and width 3).
+ *  axis_of_pair : the axis whose position turns pair i, i < rot_dim/2. */
+#define POT_MAX_AXES 4
+typedef struct pot_rope {
+  int32_t head_dim;
+  int32_t rot_dim;
+  int32_t neighbours;
+  int32_t n_axes;
+  uint8_t axis_of_pair[32];
+} pot_rope;
+
+/* The rows of one part of a projection: element m of head h of token t of batch row
+ * b is data[b * stride_b + t * stride_s + h * stride_h + m] (strides in elements; 0 or
+ * negative ones may be given). */
+typedef struct pot_rows {
+  const void* data;
+  int64_t stride_b, stride_s, stride_h;
+} pot_rows;
+
+/* Norm of queries and keys per head and their position rotation, in one pass from
+ * the rows of a QKV projection to what the cache writers and the decode calls take:
+ *    y = x / sqrt(mean x^2 + eps) * w             (where there are weights w)
+ *    (a, b) -> (a cos f - b sin f, b cos f + a sin f), f = position * inv_freq[i],
+ * for pair i with the position on its axis. Values v pass as they are. All in fp32
+ * (the angle in fp64, so that far positions keep their place in the turn), one
+ * rounding at the end.
+ *  dtype        pot_dtype of q, k and v.
+ *  q, k, v      host structs of device rows: [B][S][Hq], [B][S][Hkv] and [B][S][Hkv]
+ *               rows of 64 elements, e.g. the parts of one packed projection. A NULL
+ *               struct or data leaves the part out; its output must then be NULL too.
+ *               Rows must be 16-byte aligned (data, and the strides of dimensions
+ *               over 1).
+ *  q_weight, k_weight [64] of weight_dtype, device, or NULL: no norm of that part.
+ *  eps          finite, >= 0.
+ *  positions    int64 [n_axes][B][S], device, any sign (8-byte aligned; NULL iff
+ *               rot_dim = 0). The angle is exact to 2^-52 of itself plus rounding: for
+ *               |position * inv_freq| up to 2^31 within 1e-6.
+ *  inv_freq     double [rot_dim/2], device: radians per position (NULL iff rot_dim = 0).
+ *  q_out        [B][Hq][S][64] of q_out_dtype (pot_decode_attention takes fp32 with
+ *               S = 1).
+ *  k_out, v_out fp16 [B][Hkv][S][64] (dense rows for pot_encode_keys and the value
+ *               stores; S = 1: k_new and v_new of the append calls).
+ * Outputs are 16-byte aligned and alias nothing. B or S of 0 is a no-op. */
+pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
+                         const pot_rows* k, const pot_rows* v, const void* q_weight,
+                         const void* k_weight, int32_t weight_dtype, float eps,
+                         const int64_t* positions, const double* inv_freq, int32_t B, int32_t S,
+                         int32_t Hq, int32_t Hkv, int32_t q_out_dtype, void* q_out,
+                         uint16_t* k_out, uint16_t* v_out, void* stream);
+
 /* Workspace bytes pot_decode_attention needs for this problem shape: the
  * key-split partials (M_s, l_s, o_s) for the largest split count the planner
  * can choose, and room of each (batch, kv head, split) at its head, of which
@@ -343,6 +445,43 @@ pot_status pot_append_decode_attention_v8(const pot_format* fmt, int32_t engine,
                                           int32_t Hq, int32_t Hkv, int32_t T, float* out,
                                           void* workspace, size_t ws_bytes,
                                           pot_debug* dbg, void* stream);
+
+/* Decode attention over a cache held in 4 bits: PoT keys and the values of
+ * pot_store_values_int4 (PoT-4: 72 bytes per key and value against 101 with INT8 and
+ * 164 with fp16 values).
+ *    O = sum_t p_t (z_t + s_t n_t) / sum_t p_t
+ * with the weights p of pot_decode_attention. The weights p_t s_t go to the matrix
+ * cores as fp16 high and low parts, the codes as the fp16 numbers n_t - 8 (exact), sums
+ * are fp32; p_t (z_t + 8 s_t) is summed in fp32 beside them.
+ *  engine    as pot_decode_attention_v8.
+ *  v_u4      [B*Hkv][t_cap/8][POT_INT4_GROUP_BYTES], 16-byte aligned.
+ *  seq_lens  device int32 [B], or NULL: sequence b attends over its first
+ *            seq_lens[b] keys instead of T (values are taken into 0 .. T; T is then
+ *            the longest length that may occur, which the key splits are planned
+ *            for). A sequence without keys gets O = 0. Rows past a sequence's length
+ *            never reach O.
+ * Other arguments, workspace and errors as pot_decode_attention_v8; of dbg only
+ * the launch controls and events (a tap -> POT_ERR_UNSUPPORTED); split_len is
+ * reported for length T. */
+pot_status pot_decode_attention_v4(const pot_format* fmt, int32_t engine, const float* q,
+                                   const uint8_t* codes_se, const uint8_t* codes_m,
+                                   const float* key_scale, const uint8_t* v_u4, int64_t t_cap,
+                                   const int32_t* seq_lens, const int32_t* kv_head_of_q, int32_t B,
+                                   int32_t Hq, int32_t Hkv, int32_t T, float* out, void* workspace,
+                                   size_t ws_bytes, pot_debug* dbg, void* stream);
+
+/* pot_append_decode_attention on such a cache: the new token of every sequence is
+ * encoded and quantised (as pot_encode_keys and pot_store_values_int4 do) into its
+ * last row, T - 1 or seq_lens[b] - 1, and pot_decode_attention_v4 runs over the keys
+ * with it, in one call. A sequence of length 0 takes nothing in. Arguments and errors
+ * as the calls it combines. */
+pot_status pot_append_decode_attention_v4(const pot_format* fmt, int32_t engine, const float* q,
+                                          const uint16_t* k_new, const uint16_t* v_new,
+                                          uint8_t* codes_se, uint8_t* codes_m, float* key_scale,
+                                          uint8_t* v_u4, int64_t t_cap, const int32_t* seq_lens,
+                                          const int32_t* kv_head_of_q, int32_t B, int32_t Hq,
+                                          int32_t Hkv, int32_t T, float* out, void* workspace,
+                                          size_t ws_bytes, pot_debug* dbg, void* stream);
 
 /* Bytes of the static device scratch behind pot_decode_attention_noalloc
  * (one copy per GPU, held until the process ends). */

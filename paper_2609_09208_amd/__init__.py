@@ -49,6 +49,30 @@ class pot_debug(ctypes.Structure):
                 ("force_wg_waves", ctypes.c_int32), ("wg_waves", ctypes.c_int32)]
 
 
+class pot_rope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("neighbours", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis_of_pair", ctypes.c_uint8 * 32)]
+
+
+class pot_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_s", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+POT_FP16, POT_BF16, POT_FP32 = 0, 1, 2
+POT_INT4_GROUP_BYTES = 288
+
+
+def make_rope(rot_dim: int = HEAD_DIM, neighbours: bool = False, axis_of_pair=None,
+              head_dim: int = HEAD_DIM) -> pot_rope:
+    """Rotation of a head's first rot_dim elements; axis_of_pair: the position axis of
+    each of its rot_dim/2 pairs (None: one axis)."""
+    axes = [0] * (rot_dim // 2) if axis_of_pair is None else [int(a) for a in axis_of_pair]
+    return pot_rope(head_dim, rot_dim, int(bool(neighbours)), max(axes, default=0) + 1,
+                    (ctypes.c_uint8 * 32)(*axes))
+
+
 def make_format(mant_bits: int = 0, frac_bits: int = 7, hadamard: bool = False,
                 exp_bits: int = 3, head_dim: int = HEAD_DIM) -> pot_format:
     return pot_format(head_dim, exp_bits, mant_bits, frac_bits, int(bool(hadamard)))
@@ -67,6 +91,7 @@ def _load_library():
     i32, i64 = ctypes.c_int32, ctypes.c_int64
     fmt_p = ctypes.POINTER(pot_format)
     dbg_p = ctypes.POINTER(pot_debug)
+    rows_p = ctypes.POINTER(pot_rows)
     sig = {
         "pot_status_string": (ctypes.c_char_p, [i32]),
         "pot_last_error": (ctypes.c_char_p, []),
@@ -93,6 +118,17 @@ def _load_library():
                                             S, dbg_p, P]),
         "pot_dot_decode_attention": (i32, [fmt_p, P, P, P, P, P, i64, P, i32, i32, i32, i32,
                                            P, P, S, dbg_p, P]),
+        "pot_decode_attention_v4": (i32, [fmt_p, i32, P, P, P, P, P, i64, P, P, i32, i32, i32,
+                                          i32, P, P, S, dbg_p, P]),
+        "pot_append_decode_attention_v4": (i32, [fmt_p, i32, P, P, P, P, P, P, P, i64, P, P, i32,
+                                                 i32, i32, i32, P, P, S, dbg_p, P]),
+        "pot_store_values_int4": (i32, [P, i64, i64, i64, i64, P, P]),
+        "pot_load_keys": (i32, [fmt_p, P, P, P, i64, i64, i64, i64, P, P]),
+        "pot_load_values": (i32, [P, i64, i64, i64, i64, P, P]),
+        "pot_load_values_int8": (i32, [P, P, i64, i64, i64, i64, P, P]),
+        "pot_load_values_int4": (i32, [P, i64, i64, i64, i64, P, P]),
+        "pot_norm_rope": (i32, [ctypes.POINTER(pot_rope), i32, rows_p, rows_p, rows_p, P, P, i32,
+                                ctypes.c_float, P, P, i32, i32, i32, i32, i32, P, P, P, P]),
         "pot_int8_encode_keys": (i32, [P, i64, i64, i32, P, P, P]),
         "pot_int8_decode_attention": (i32, [P, P, P, P, i64, P, i32, i32, i32,
                                             i32, i32, P, P, S, dbg_p, P]),
@@ -274,6 +310,116 @@ def pot_append_decode_attention_v8(fmt: pot_format, engine: int, q, k_new, v_new
         _stream(stream)))
 
 
+def pot_store_values_int4(v_fp16, n_seq: int, n_tok: int, t_cap: int, t0: int, v_u4,
+                          stream=None) -> None:
+    _check(_lib.pot_store_values_int4(_ptr(v_fp16), int(n_seq), int(n_tok), int(t_cap),
+                                      int(t0), _ptr(v_u4), _stream(stream)))
+
+
+def pot_load_keys(fmt: pot_format, codes_se, codes_m, key_scale, n_seq: int, n_tok: int,
+                  t_cap: int, t0: int, k_fp16, stream=None) -> None:
+    _check(_lib.pot_load_keys(ctypes.byref(fmt), _ptr(codes_se), _ptr(codes_m), _ptr(key_scale),
+                              int(n_seq), int(n_tok), int(t_cap), int(t0), _ptr(k_fp16),
+                              _stream(stream)))
+
+
+def pot_load_values(v_cache, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp16,
+                    stream=None) -> None:
+    _check(_lib.pot_load_values(_ptr(v_cache), int(n_seq), int(n_tok), int(t_cap), int(t0),
+                                _ptr(v_fp16), _stream(stream)))
+
+
+def pot_load_values_int8(v_u8, v_exp, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp16,
+                         stream=None) -> None:
+    _check(_lib.pot_load_values_int8(_ptr(v_u8), _ptr(v_exp), int(n_seq), int(n_tok), int(t_cap),
+                                     int(t0), _ptr(v_fp16), _stream(stream)))
+
+
+def pot_load_values_int4(v_u4, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp16,
+                         stream=None) -> None:
+    _check(_lib.pot_load_values_int4(_ptr(v_u4), int(n_seq), int(n_tok), int(t_cap), int(t0),
+                                     _ptr(v_fp16), _stream(stream)))
+
+
+def pot_decode_attention_v4(fmt: pot_format, engine: int, q, codes_se, codes_m, key_scale, v_u4,
+                            t_cap: int, seq_lens, kv_head_of_q, B: int, Hq: int, Hkv: int, T: int,
+                            out, workspace, ws_bytes=None, dbg: pot_debug | None = None,
+                            stream=None) -> None:
+    _, hp = _heads(kv_head_of_q)
+    nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
+    _check(_lib.pot_decode_attention_v4(
+        ctypes.byref(fmt), int(engine), _ptr(q), _ptr(codes_se), _ptr(codes_m),
+        _ptr(key_scale), _ptr(v_u4), int(t_cap), _ptr(seq_lens), hp, B, Hq, Hkv, T, _ptr(out),
+        _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
+        _stream(stream)))
+
+
+def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new, codes_se,
+                                   codes_m, key_scale, v_u4, t_cap: int, seq_lens, kv_head_of_q,
+                                   B: int, Hq: int, Hkv: int, T: int, out, workspace,
+                                   ws_bytes=None, dbg: pot_debug | None = None,
+                                   stream=None) -> None:
+    _, hp = _heads(kv_head_of_q)
+    nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
+    _check(_lib.pot_append_decode_attention_v4(
+        ctypes.byref(fmt), int(engine), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(codes_se),
+        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _ptr(seq_lens), hp, B, Hq, Hkv, T,
+        _ptr(out), _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
+        _stream(stream)))
+
+
+_DTYPES = {torch.float16: POT_FP16, torch.bfloat16: POT_BF16, torch.float32: POT_FP32}
+
+
+def _part(x, out, B: int, S: int):
+    """A part of a projection [B, S, heads, 64] (any strides, elements side by side) as
+    (pot_rows by reference or None, its heads)."""
+    if x is None:
+        return None, 0
+    H = x.shape[2]
+    sb, ss, sh, se = x.stride()
+    if (x.shape[0] != B or x.shape[1] != S or x.shape[3] != HEAD_DIM or se != 1 or out is None
+            or out.shape != (B, H, S, HEAD_DIM) or not out.is_contiguous()):
+        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG",
+                       "rows [B, S, heads, 64] with dense elements and a dense output "
+                       "[B, heads, S, 64] are needed")
+    return ctypes.byref(pot_rows(x.data_ptr(), sb, ss, sh)), H
+
+
+def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions, inv_freq,
+                  q_out, k_out, v_out, stream=None) -> None:
+    """q [B, S, Hq, 64], k and v [B, S, Hkv, 64] (tensors of one type, any strides, None:
+    left out) to q_out [B, Hq, S, 64], k_out and v_out [B, Hkv, S, 64] (dense; k_out and
+    v_out float16). positions int64 [n_axes, B, S], inv_freq float64 [rot_dim/2], weights
+    [64] of one type or None."""
+    given = [x for x in (q, k, v) if x is not None]
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if not given:
+        return
+    B, S = given[0].shape[0], given[0].shape[1]
+    (qr, hq), (kr, hk), (vr, hv) = _part(q, q_out, B, S), _part(k, k_out, B, S), _part(v, v_out, B, S)
+    dtype, wtype = given[0].dtype, weights[0].dtype if weights else torch.float32
+    qtype = q_out.dtype if q_out is not None else torch.float32
+    n_pos = rope.n_axes * B * S
+    if ((k is not None and v is not None and hk != hv) or any(x.dtype != dtype for x in given)
+            or any(w.dtype != wtype or w.shape != (HEAD_DIM,) or not w.is_contiguous()
+                   for w in weights)
+            or any(o is not None and o.dtype != torch.float16 for o in (k_out, v_out))
+            or any(t not in _DTYPES for t in (dtype, wtype, qtype))
+            or (positions is not None and (positions.dtype != torch.int64
+                                           or positions.numel() != n_pos
+                                           or not positions.is_contiguous()))
+            or (inv_freq is not None and (inv_freq.dtype != torch.float64
+                                          or inv_freq.numel() < rope.rot_dim // 2
+                                          or not inv_freq.is_contiguous()))):
+        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG",
+                       "types or shapes that do not go together")
+    _check(_lib.pot_norm_rope(
+        ctypes.byref(rope), _DTYPES[dtype], qr, kr, vr, _ptr(q_weight), _ptr(k_weight),
+        _DTYPES[wtype], float(eps), _ptr(positions), _ptr(inv_freq), B, S, hq, hk or hv,
+        _DTYPES[qtype], _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
 def pot_ds4a_decode_attention(fmt: pot_format, q, codes_se, key_scale, v_fp16, t_cap: int,
                               kv_head_of_q, B: int, Hq: int, Hkv: int, T: int, out,
                               workspace, ws_bytes=None, dbg: pot_debug | None = None,
@@ -351,6 +497,12 @@ def alloc_value_cache_int8(B: int, Hkv: int, t_cap: int, device):
     exponents int8 [B,Hkv,t_cap])."""
     return (torch.zeros((B, Hkv, t_cap, HEAD_DIM), dtype=torch.uint8, device=device),
             torch.zeros((B, Hkv, t_cap), dtype=torch.int8, device=device))
+
+
+def alloc_value_cache_int4(B: int, Hkv: int, t_cap: int, device):
+    """4-bit value cache: uint8 [B,Hkv,t_cap/8,288], records of 8 tokens."""
+    return torch.zeros((B, Hkv, t_cap // 8, POT_INT4_GROUP_BYTES), dtype=torch.uint8,
+                       device=device)
 
 
 def alloc_workspace(nbytes: int, device):

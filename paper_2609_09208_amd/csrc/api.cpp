@@ -280,7 +280,13 @@ pot_status decode_common(int mode, int mant_bits, DecodeArgs& a, const int32_t* 
   if (t_cap % 8)
     return fail(POT_ERR_INVALID_ARG, "t_cap %lld is not a multiple of 8 (value-cache groups)",
                 (long long)t_cap);
-  if (v8) {
+  if (vf == 3) {
+    if (!a.q || !a.v4 || !a.out) return fail(POT_ERR_INVALID_ARG, "q, v_u4 or out is NULL");
+    if (!aligned(a.q, 16) || !aligned(a.v4, 16) || !aligned(a.out, 16))
+      return fail(POT_ERR_INVALID_ARG, "q, v_u4 and out must be 16-byte aligned");
+    if (!aligned(a.seq_lens, 4))
+      return fail(POT_ERR_INVALID_ARG, "seq_lens must be 4-byte aligned");
+  } else if (v8) {
     if (!a.q || !a.v8 || !a.v_exp || !a.out)
       return fail(POT_ERR_INVALID_ARG, "q, v_u8, v_exp or out is NULL");
     if (!aligned(a.q, 16) || !aligned(a.v8, 16) || !aligned(a.v_exp, 16) || !aligned(a.out, 16))
@@ -353,6 +359,8 @@ pot_status decode_common(int mode, int mant_bits, DecodeArgs& a, const int32_t* 
     dbg->wg_waves = a.wg_waves;
     if (debug && mode == kScoreFp16)
       return fail(POT_ERR_UNSUPPORTED, "debug taps are not available on the fp16 path");
+    if (debug && vf == 3)
+      return fail(POT_ERR_UNSUPPORTED, "debug taps are not available with 4-bit values");
   }
   return hip_status(
       launch_decode(mode, G, mant_bits, debug, vf, a, static_cast<hipStream_t>(stream), ev_begin,
@@ -392,6 +400,99 @@ pot_status decode_v8(int vf, const pot_format* fmt, int32_t engine, const float*
   a.hadamard = fmt->hadamard;
   return decode_common(engine == 0 ? kScorePot : kScoreDs4a, fmt->mant_bits, a, kv_head_of_q, B,
                        Hq, Hkv, T, t_cap, workspace, ws_bytes, dbg, stream, vf);
+}
+
+// Shared body of the 4-bit-value entry points; append: k_new and v_new are taken in.
+pot_status decode_v4(bool append, const pot_format* fmt, int32_t engine, const float* q,
+                     const uint16_t* k_new, const uint16_t* v_new, const uint8_t* codes_se,
+                     const uint8_t* codes_m, const float* key_scale, const uint8_t* v_u4,
+                     int64_t t_cap, const int32_t* seq_lens, const int32_t* kv_head_of_q,
+                     int32_t B, int32_t Hq, int32_t Hkv, int32_t T, float* out, void* workspace,
+                     size_t ws_bytes, pot_debug* dbg, void* stream) {
+  pot_status st = check_format(fmt);
+  if (st != POT_OK) return st;
+  if (engine != 0 && engine != 1)
+    return fail(POT_ERR_INVALID_ARG, "engine %d (0 shift-accumulate, 1 byte decode)", engine);
+  if (engine == 1 && fmt->mant_bits != 0)
+    return fail(POT_ERR_UNSUPPORTED, "the byte-decode path scores PoT-4 codes only (mant_bits 0)");
+  if (append && (!k_new || !v_new)) return fail(POT_ERR_INVALID_ARG, "k_new or v_new is NULL");
+  if (append && (!aligned(k_new, 16) || !aligned(v_new, 16)))
+    return fail(POT_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+  if (!codes_se || !key_scale) return fail(POT_ERR_INVALID_ARG, "codes_se or key_scale is NULL");
+  if ((fmt->mant_bits > 0) != (codes_m != nullptr))
+    return fail(POT_ERR_INVALID_ARG, "codes_m must be non-NULL exactly when mant_bits > 0");
+  if (!aligned(codes_se, 16) || !aligned(key_scale, 4) || (codes_m && !aligned(codes_m, 8)))
+    return fail(POT_ERR_INVALID_ARG, "misaligned codes_se / key_scale / codes_m");
+  DecodeArgs a{};
+  a.q = q;
+  a.codes_se = codes_se;
+  a.codes_m = codes_m;
+  a.key_scale = key_scale;
+  a.v4 = v_u4;
+  a.seq_lens = seq_lens;
+  a.out = out;
+  a.frac_bits = fmt->frac_bits;
+  a.hadamard = fmt->hadamard;
+  if (append) {
+    a.app_k = k_new;
+    a.app_v = v_new;
+    a.app_codes_se = const_cast<uint8_t*>(codes_se);
+    a.app_codes_m = const_cast<uint8_t*>(codes_m);
+    a.app_key_scale = const_cast<float*>(key_scale);
+    a.app_v4 = const_cast<uint8_t*>(v_u4);
+    a.app_tab = encode_tables(fmt->mant_bits);
+  }
+  return decode_common(engine == 0 ? kScorePot : kScoreDs4a, fmt->mant_bits, a, kv_head_of_q, B,
+                       Hq, Hkv, T, t_cap, workspace, ws_bytes, dbg, stream, 3);
+}
+
+// Rows [t0, t0 + n_tok) of n_seq sequences of t_cap rows.
+pot_status check_rows(int64_t n_seq, int64_t n_tok, int64_t t_cap, int64_t t0) {
+  if (n_seq < 0 || n_tok < 0)
+    return fail(POT_ERR_INVALID_ARG, "n_seq %lld / n_tok %lld < 0", (long long)n_seq,
+                (long long)n_tok);
+  if (t_cap < 8 || t_cap % 8)
+    return fail(POT_ERR_INVALID_ARG, "t_cap %lld is not a positive multiple of 8",
+                (long long)t_cap);
+  if (t0 < 0 || n_tok > t_cap || t0 > t_cap - n_tok)
+    return fail(POT_ERR_INVALID_ARG, "n_tok %lld tokens from %lld outside [0, t_cap = %lld)",
+                (long long)n_tok, (long long)t0, (long long)t_cap);
+  if (n_tok > 0 && n_seq > ((int64_t)1 << 31) / n_tok)
+    return fail(POT_ERR_INVALID_ARG, "n_seq * n_tok too large");
+  return POT_OK;
+}
+
+pot_status load_values(int format, const void* cache, const int8_t* v_exp, int64_t n_seq,
+                       int64_t n_tok, int64_t t_cap, int64_t t0, uint16_t* v_fp16, void* stream) {
+  pot_status st = check_rows(n_seq, n_tok, t_cap, t0);
+  if (st != POT_OK) return st;
+  if (n_seq == 0 || n_tok == 0) return ok();
+  if (!cache || !v_fp16 || (format == 1 && !v_exp))
+    return fail(POT_ERR_INVALID_ARG, "a value cache pointer or v_fp16 is NULL");
+  if (!aligned(cache, 16) || !aligned(v_fp16, 16) || !aligned(v_exp, 16))
+    return fail(POT_ERR_INVALID_ARG, "the value cache and v_fp16 must be 16-byte aligned");
+  return hip_status(launch_load_values(format, cache, v_exp, n_seq, n_tok, t_cap, t0, v_fp16,
+                                       static_cast<hipStream_t>(stream)),
+                    "load values launch");
+}
+
+// One part of a projection and its output: both given, or neither.
+pot_status check_part(const char* name, const pot_rows* r, const void* out, int32_t heads,
+                      int32_t B, int32_t S, int size, RowsIn* in) {
+  *in = RowsIn{};
+  if (!r || !r->data) {
+    if (out) return fail(POT_ERR_INVALID_ARG, "%s is left out, but not its output", name);
+    return POT_OK;
+  }
+  if (!out) return fail(POT_ERR_INVALID_ARG, "%s has no output", name);
+  if (heads < 1) return fail(POT_ERR_INVALID_ARG, "%d heads of %s", heads, name);
+  const int64_t per16 = 16 / size;
+  if (!aligned(r->data, 16) || !aligned(out, 16) || (B > 1 && r->stride_b % per16) ||
+      (S > 1 && r->stride_s % per16) || (heads > 1 && r->stride_h % per16))
+    return fail(POT_ERR_INVALID_ARG, "rows of %s and its output must be 16-byte aligned", name);
+  *in = RowsIn{r->data, B > 1 ? r->stride_b : 0, S > 1 ? r->stride_s : 0,
+               heads > 1 ? r->stride_h : 0};
+  return POT_OK;
 }
 
 }  // namespace
@@ -484,6 +585,120 @@ pot_status pot_store_values_int8(const uint16_t* v_fp16, int64_t n_seq, int64_t 
   return hip_status(launch_store_values_i8(v_fp16, n_seq, n_tok, t_cap, t0, v_u8, v_exp,
                                            static_cast<hipStream_t>(stream)),
                     "store values launch");
+}
+
+pot_status pot_store_values_int4(const uint16_t* v_fp16, int64_t n_seq, int64_t n_tok,
+                                 int64_t t_cap, int64_t t0, uint8_t* v_u4, void* stream) {
+  pot_status st = check_rows(n_seq, n_tok, t_cap, t0);
+  if (st != POT_OK) return st;
+  if (n_seq == 0 || n_tok == 0) return ok();
+  if (!v_fp16 || !v_u4) return fail(POT_ERR_INVALID_ARG, "v_fp16 or v_u4 is NULL");
+  if (!aligned(v_fp16, 16) || !aligned(v_u4, 16))
+    return fail(POT_ERR_INVALID_ARG, "v_fp16 and v_u4 must be 16-byte aligned");
+  return hip_status(launch_store_values_i4(v_fp16, n_seq, n_tok, t_cap, t0, v_u4,
+                                           static_cast<hipStream_t>(stream)),
+                    "store values launch");
+}
+
+pot_status pot_load_keys(const pot_format* fmt, const uint8_t* codes_se, const uint8_t* codes_m,
+                         const float* key_scale, int64_t n_seq, int64_t n_tok, int64_t t_cap,
+                         int64_t t0, uint16_t* k_fp16, void* stream) {
+  pot_status st = check_format(fmt);
+  if (st != POT_OK) return st;
+  st = check_rows(n_seq, n_tok, t_cap, t0);
+  if (st != POT_OK) return st;
+  if (n_seq == 0 || n_tok == 0) return ok();
+  if (!codes_se || !key_scale || !k_fp16)
+    return fail(POT_ERR_INVALID_ARG, "codes_se, key_scale or k_fp16 is NULL");
+  if ((fmt->mant_bits > 0) != (codes_m != nullptr))
+    return fail(POT_ERR_INVALID_ARG, "codes_m must be non-NULL exactly when mant_bits > 0");
+  if (!aligned(codes_se, 16) || !aligned(key_scale, 4) || !aligned(k_fp16, 16) ||
+      (codes_m && !aligned(codes_m, 8)))
+    return fail(POT_ERR_INVALID_ARG, "misaligned codes_se / key_scale / codes_m / k_fp16");
+  return hip_status(launch_load_keys(fmt->mant_bits, fmt->hadamard, codes_se, codes_m, key_scale,
+                                     n_seq, n_tok, t_cap, t0, k_fp16,
+                                     static_cast<hipStream_t>(stream)),
+                    "load keys launch");
+}
+
+pot_status pot_load_values(const uint16_t* v_cache, int64_t n_seq, int64_t n_tok, int64_t t_cap,
+                           int64_t t0, uint16_t* v_fp16, void* stream) {
+  return load_values(0, v_cache, nullptr, n_seq, n_tok, t_cap, t0, v_fp16, stream);
+}
+
+pot_status pot_load_values_int8(const uint8_t* v_u8, const int8_t* v_exp, int64_t n_seq,
+                                int64_t n_tok, int64_t t_cap, int64_t t0, uint16_t* v_fp16,
+                                void* stream) {
+  return load_values(1, v_u8, v_exp, n_seq, n_tok, t_cap, t0, v_fp16, stream);
+}
+
+pot_status pot_load_values_int4(const uint8_t* v_u4, int64_t n_seq, int64_t n_tok, int64_t t_cap,
+                                int64_t t0, uint16_t* v_fp16, void* stream) {
+  return load_values(2, v_u4, nullptr, n_seq, n_tok, t_cap, t0, v_fp16, stream);
+}
+
+pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
+                         const pot_rows* k, const pot_rows* v, const void* q_weight,
+                         const void* k_weight, int32_t weight_dtype, float eps,
+                         const int64_t* positions, const double* inv_freq, int32_t B, int32_t S,
+                         int32_t Hq, int32_t Hkv, int32_t q_out_dtype, void* q_out,
+                         uint16_t* k_out, uint16_t* v_out, void* stream) {
+  if (!rope) return fail(POT_ERR_INVALID_ARG, "rope is NULL");
+  if (rope->head_dim != 64)
+    return fail(POT_ERR_UNSUPPORTED, "head_dim %d (only 64)", rope->head_dim);
+  const int r = rope->rot_dim;
+  if (r < 0 || r > 64 || r % 2)
+    return fail(POT_ERR_INVALID_ARG, "rot_dim %d (even, 0 .. 64)", r);
+  if (rope->neighbours != 0 && rope->neighbours != 1)
+    return fail(POT_ERR_INVALID_ARG, "neighbours %d (0 or 1)", rope->neighbours);
+  if (rope->n_axes < 1 || rope->n_axes > POT_MAX_AXES)
+    return fail(POT_ERR_INVALID_ARG, "n_axes %d (1 .. %d)", rope->n_axes, POT_MAX_AXES);
+  for (int i = 0; i < r / 2; ++i)
+    if (rope->axis_of_pair[i] >= rope->n_axes)
+      return fail(POT_ERR_INVALID_ARG, "axis_of_pair[%d] = %d outside [0, %d)", i,
+                  rope->axis_of_pair[i], rope->n_axes);
+  for (const int32_t t : {dtype, weight_dtype, q_out_dtype})
+    if (t < POT_FP16 || t > POT_FP32)
+      return fail(POT_ERR_INVALID_ARG, "type %d (0 fp16, 1 bf16, 2 fp32)", t);
+  if (!(eps >= 0.0f && eps <= 3.4e38f)) return fail(POT_ERR_INVALID_ARG, "eps %g", eps);
+  if (B < 0 || S < 0 || Hq < 0 || Hkv < 0)
+    return fail(POT_ERR_INVALID_ARG, "bad shape B=%d S=%d Hq=%d Hkv=%d", B, S, Hq, Hkv);
+  if (B == 0 || S == 0) return ok();
+  NormRopeArgs a{};
+  const int size = dtype == POT_FP32 ? 4 : 2;
+  pot_status st = check_part("q", q, q_out, Hq, B, S, size, &a.q);
+  if (st == POT_OK) st = check_part("k", k, k_out, Hkv, B, S, size, &a.k);
+  if (st == POT_OK) st = check_part("v", v, v_out, Hkv, B, S, size, &a.v);
+  if (st != POT_OK) return st;
+  if (!a.q.data && !a.k.data && !a.v.data) return ok();
+  if (r > 0 && (a.q.data || a.k.data) && (!positions || !inv_freq))
+    return fail(POT_ERR_INVALID_ARG, "positions or inv_freq is NULL");
+  if (!aligned(positions, 8) || !aligned(inv_freq, 8))
+    return fail(POT_ERR_INVALID_ARG, "positions and inv_freq must be 8-byte aligned");
+  const size_t w_size = weight_dtype == POT_FP32 ? 4 : 2;
+  if (!aligned(q_weight, w_size) || !aligned(k_weight, w_size))
+    return fail(POT_ERR_INVALID_ARG, "misaligned q_weight / k_weight");
+  if ((int64_t)B * S > ((int64_t)1 << 31))
+    return fail(POT_ERR_INVALID_ARG, "B * S too large");
+  a.q_weight = a.q.data ? q_weight : nullptr;
+  a.k_weight = a.k.data ? k_weight : nullptr;
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.eps = eps;
+  a.B = B;
+  a.S = S;
+  a.Hq = a.q.data ? Hq : 0;
+  a.Hkv = a.k.data || a.v.data ? Hkv : 0;
+  a.dtype = dtype;
+  a.weight_dtype = weight_dtype;
+  a.q_out_dtype = q_out_dtype;
+  a.rot_dim = r;
+  a.neighbours = rope->neighbours;
+  for (int i = 0; i < 32; ++i) a.axis_of_pair[i] = i < r / 2 ? rope->axis_of_pair[i] : 0;
+  return hip_status(launch_norm_rope(a, static_cast<hipStream_t>(stream)), "norm and rotation launch");
 }
 
 size_t pot_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t T) {
@@ -631,6 +846,28 @@ pot_status pot_append_decode_attention_v8(const pot_format* fmt, int32_t engine,
   a.app_tab = encode_tables(fmt->mant_bits);
   return decode_common(engine == 0 ? kScorePot : kScoreDs4a, fmt->mant_bits, a, kv_head_of_q, B,
                        Hq, Hkv, T, t_cap, workspace, ws_bytes, dbg, stream, 1);
+}
+
+pot_status pot_decode_attention_v4(const pot_format* fmt, int32_t engine, const float* q,
+                                   const uint8_t* codes_se, const uint8_t* codes_m,
+                                   const float* key_scale, const uint8_t* v_u4, int64_t t_cap,
+                                   const int32_t* seq_lens, const int32_t* kv_head_of_q, int32_t B,
+                                   int32_t Hq, int32_t Hkv, int32_t T, float* out, void* workspace,
+                                   size_t ws_bytes, pot_debug* dbg, void* stream) {
+  return decode_v4(false, fmt, engine, q, nullptr, nullptr, codes_se, codes_m, key_scale, v_u4,
+                   t_cap, seq_lens, kv_head_of_q, B, Hq, Hkv, T, out, workspace, ws_bytes, dbg,
+                   stream);
+}
+
+pot_status pot_append_decode_attention_v4(const pot_format* fmt, int32_t engine, const float* q,
+                                          const uint16_t* k_new, const uint16_t* v_new,
+                                          uint8_t* codes_se, uint8_t* codes_m, float* key_scale,
+                                          uint8_t* v_u4, int64_t t_cap, const int32_t* seq_lens,
+                                          const int32_t* kv_head_of_q, int32_t B, int32_t Hq,
+                                          int32_t Hkv, int32_t T, float* out, void* workspace,
+                                          size_t ws_bytes, pot_debug* dbg, void* stream) {
+  return decode_v4(true, fmt, engine, q, k_new, v_new, codes_se, codes_m, key_scale, v_u4, t_cap,
+                   seq_lens, kv_head_of_q, B, Hq, Hkv, T, out, workspace, ws_bytes, dbg, stream);
 }
 
 pot_status pot_ds4a_decode_attention(const pot_format* fmt, const float* q,

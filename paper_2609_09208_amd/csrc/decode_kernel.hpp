@@ -142,12 +142,21 @@ struct KeyRegs<kScoreFp16, K> {
   uint4 k[2][4];
 };
 
-template <bool V8>
+// How a value format (VF, below) holds its values.
+enum ValueKind : int { kValF16 = 0, kValI8 = 1, kValI4 = 2 };
+constexpr int value_kind(int vf) { return vf == 0 ? kValF16 : vf == 3 ? kValI4 : kValI8; }
+
+template <int VK>
 struct ValRegs {
   uint4 f[2][4];  // [K-block of 32 keys][16-dim block], 8 fp16 values each
 };
 template <>
-struct ValRegs<true> {
+struct ValRegs<kValI4> {
+  uint4 f[2];  // [K-block]: the fragments of all four 16-dim blocks, a half byte per value
+  uint4 s, z;  // fp16 steps and minima of the 8 keys whose weights this lane forms
+};
+template <>
+struct ValRegs<kValI8> {
   uint2 f[2][4];  // the same fragments as 8 value bytes (v^ + 128)
   uint2 g;        // exponents g of the 8 keys whose weights this lane forms
 };
@@ -260,9 +269,26 @@ __device__ __forceinline__ void plane_bits(const KeyRegs<MODE, K>& r, int s, uin
 // the lane also loads the exponents of the 8 keys t0 + 32*part + 8*grp ..+7
 // whose weights it forms in stage 2.
 // Blocks kFirst .. kEnd - 1 of the two K-blocks; the exponents come with block 0.
-template <bool V8, int kFirst = 0, int kEnd = 2>
+// 4-bit values: one 16-byte load per K-block holds the lane's fragments of all four
+// dimension blocks (pot_device.hpp, value_byte_i4), and the steps and minima of the 8
+// keys whose weights the lane forms stand behind the values of their group.
+template <int VK, int kFirst = 0, int kEnd = 2>
 __device__ __forceinline__ void load_values_buf(const Streams& st, int t0, int lane,
-                                                ValRegs<V8>& v) {
+                                                ValRegs<VK>& v) {
+  constexpr bool V8 = VK == kValI8;
+  if constexpr (VK == kValI4) {
+    const BufRsrc rv = tile_rsrc(st.values, t0, st.v_end, kI4GroupBytes / 8);
+    const int part = (lane & 15) >> 3, grp = lane >> 4;
+    const int voff = tile_offset(grp * kI4GroupBytes + (lane & 15) * 16, t0);
+#pragma unroll
+    for (int kb = kFirst; kb < kEnd; ++kb) v.f[kb] = load_b128(rv, voff + kb * 4 * kI4GroupBytes, true);
+    if constexpr (kFirst == 0) {
+      const int soff = tile_offset((4 * part + grp) * kI4GroupBytes + kI4Steps, t0);
+      v.s = load_b128(rv, soff, false);
+      v.z = load_b128(rv, soff + kI4Minima - kI4Steps, false);
+    }
+    return;
+  } else {
   constexpr int kGroupBytes = V8 ? 8 * kDim : 16 * kDim;  // one 8-token group
   const BufRsrc rv = tile_rsrc(st.values, t0, st.v_end, kGroupBytes / 8);
   const int voff = tile_offset((lane >> 4) * kGroupBytes + (lane & 15) * (V8 ? 8 : 16), t0);
@@ -287,6 +313,56 @@ __device__ __forceinline__ void load_values_buf(const Streams& st, int t0, int l
         __builtin_amdgcn_raw_buffer_load_b64(re, tile_offset(32 * part + 8 * grp, t0), 0, 0);
     v.g = make_uint2(g.x, g.y);
   }
+  }
+}
+
+// fp16 B fragment of 8 4-bit values as the numbers n - 8 (exact). w0, w1: the bytes of 8
+// tokens, each the n of dimension block 2 h in its low half and of block 2 h + 1 in its
+// high half. Half bytes put under the fp16 exponent byte 0x64 are the numbers 1024 + n
+// or 1024 + 16 n; a packed addition or multiply-add takes them to n - 8. The tokens come
+// out in the order 0 2 1 3 4 6 5 7. (The half bytes as they are, subnormal fp16 numbers,
+// would take no arithmetic, but the matrix cores do not normalise them: products lose
+// up to 10 bits, 7e-5 of the value scale where this has 2e-7; 1024 + n without the
+// addition, its constant taken off the sums, cancels as much.)
+struct NibbleConst {
+  uint32_t even, odd, exp;  // in VGPRs, as m22 in the kernel
+};
+template <bool ODD>
+__device__ __forceinline__ half8 int4_value_fragment(uint32_t w0, uint32_t w1,
+                                                     const NibbleConst& k) {
+  const uint32_t w[4] = {w0, w0 >> 8, w1, w1 >> 8};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const half2v v = __builtin_bit_cast(
+        half2v, __builtin_amdgcn_bitop3_b32(w[i], ODD ? k.odd : k.even, k.exp, kMaskOrTable));
+    const half2v c = {(_Float16)(ODD ? -72.0f : -1032.0f), (_Float16)(ODD ? -72.0f : -1032.0f)};
+    const half2v f = {(_Float16)0.0625f, (_Float16)0.0625f};
+    r[i] = __builtin_bit_cast(uint32_t, ODD ? __builtin_elementwise_fma(v, f, c) : v + c);
+  }
+  return __builtin_bit_cast(half8, make_uint4(r[0], r[1], r[2], r[3]));
+}
+
+// Steps and minima of keys at or past t_end to 0 (tail tile only): whatever the cache
+// holds there cannot reach the sums (value bits are finite numbers in any case).
+__device__ __forceinline__ void mask_steps(int k0, int t_end, ValRegs<kValI4>& v) {
+  uint32_t s[4] = {v.s.x, v.s.y, v.s.z, v.s.w}, z[4] = {v.z.x, v.z.y, v.z.z, v.z.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = ((k0 + 2 * i < t_end) ? 0x0000FFFFu : 0u) |
+                       ((k0 + 2 * i + 1 < t_end) ? 0xFFFF0000u : 0u);
+    s[i] &= m;
+    z[i] &= m;
+  }
+  v.s = make_uint4(s[0], s[1], s[2], s[3]);
+  v.z = make_uint4(z[0], z[1], z[2], z[3]);
+}
+
+// Larger of two pairs of non-negative fp16 numbers, by their bits.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                __builtin_bit_cast(u16x2, b)));
 }
 
 // fp16 B fragment of 8 INT8 values held as v^ + 128: bytes u become the fp16
@@ -308,7 +384,7 @@ __device__ __forceinline__ half8 int8_value_fragment(uint2 w) {
 
 // Zero the value fragments of tokens at or past t_end (tail tile only), so
 // that whatever the cache holds there cannot reach the sums (p is 0 there).
-__device__ __forceinline__ void mask_values(int t0, int t_end, int lane, ValRegs<false>& v) {
+__device__ __forceinline__ void mask_values(int t0, int t_end, int lane, ValRegs<kValF16>& v) {
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     const int g8 = t0 + 32 * kb + 8 * (lane >> 4);
@@ -325,6 +401,14 @@ __device__ __forceinline__ void mask_values(int t0, int t_end, int lane, ValRegs
     }
   }
 }
+
+// Sums of the weights times the values' minima, per wave and head (4-bit values).
+template <int VK, int NW>
+struct MinimaSums {};
+template <int NW>
+struct MinimaSums<kValI4, NW> {
+  float z[NW][8];
+};
 
 // ---- shared memory of the decode kernel -------------------------------------
 template <int NW>
@@ -354,22 +438,26 @@ struct DecodeSmem<kScoreInt8, NW> : MergeSmem<NW> {
 };
 
 // The new token of one (batch, kv head) sequence appended at row T - 1
-// (Sec. II-F, a cache that holds only codes): wave 0 encodes the key with the
-// row absmax scale, wave 1 stores the values (fp16, or INT8 with their
-// exponent). Only the workgroup whose key range holds row T - 1 calls it.
+// (Sec. II-F, a cache that holds only codes; T: the sequence's keys with it): wave 0
+// encodes the key with the row absmax scale, wave 1 stores the values (fp16, INT8 with
+// their exponent, or 4 bits). Only the workgroup whose key range holds row T - 1 calls it.
 // Returns the exponent of INT8 values in wave 1, INT_MAX elsewhere.
-template <int K>
-__device__ __forceinline__ int append_token(const DecodeArgs& a, int64_t seq, int wave) {
-  const int64_t row = seq * a.t_cap + (a.T - 1);
+template <int K, int VK>
+__device__ __forceinline__ int append_token(const DecodeArgs& a, int64_t seq, int wave, int T) {
+  const int64_t row = seq * a.t_cap + (T - 1);
   if (wave == 0)
     encode_key_row_wave<K>(reinterpret_cast<const __half*>(a.app_k) + seq * kDim, a.hadamard, 0,
                         a.app_key_scale + row, a.app_codes_se + row * (kDim / 2),
                         a.app_codes_m + row * 8 * K, a.app_tab);
-  else if (wave == 1 && a.app_v8 != nullptr)
+  else if constexpr (VK == kValI4) {
+    if (wave == 1)
+      store_value_token_i4_wave(a.app_v + seq * kDim, a.app_v4 + seq * a.t_cap * (kI4GroupBytes / 8),
+                                T - 1);
+  } else if (wave == 1 && a.app_v8 != nullptr)
     return store_value_token_i8_wave(a.app_v + seq * kDim, a.app_v8 + seq * a.t_cap * kDim,
-                                     a.app_v_exp + seq * a.t_cap, a.T - 1);
+                                     a.app_v_exp + seq * a.t_cap, T - 1);
   else if (wave == 1)
-    store_value_token_wave(a.app_v + seq * kDim, a.app_v_cache + seq * a.t_cap * kDim, a.T - 1);
+    store_value_token_wave(a.app_v + seq * kDim, a.app_v_cache + seq * a.t_cap * kDim, T - 1);
   return INT_MAX;
 }
 
@@ -505,7 +593,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 // lane its dimension of all splits' sums, N >= Sn of them requested together
 // (loads in a loop or behind branches wait for each other: 0.6 us a turn).
 // Splits past the last read the last one and get factor 0.
-template <int N, bool DEBUG>
+// EMPTY: sequences may hold no key; their sums are 0 and so is the output.
+__device__ __forceinline__ float quotient(float o, float l, bool empty) {
+  return empty && l == 0.0f ? 0.0f : o / l;
+}
+template <int N, bool DEBUG, bool EMPTY>
 __device__ __forceinline__ void merge_head(const DecodeArgs& a, int64_t bq, int lane) {
   const int Sn = a.n_splits, s_l = min(lane, Sn - 1);
   const int m_l = load_agent(a.part_m + bq * Sn + s_l);
@@ -523,13 +615,13 @@ __device__ __forceinline__ void merge_head(const DecodeArgs& a, int64_t bq, int 
     o = fmaf(__uint_as_float(
                  (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f_l), i)),
              v[i], o);
-  a.out[bq * kDim + lane] = o / l;
+  a.out[bq * kDim + lane] = quotient(o, l, EMPTY);
   if constexpr (DEBUG) {
     if (lane == 0 && a.dbg_m_final) a.dbg_m_final[bq] = M;
   }
 }
 
-template <int G, bool DEBUG, int NW, typename Smem>
+template <int G, bool DEBUG, bool EMPTY, int NW, typename Smem>
 __device__ __forceinline__ void merge_splits(const DecodeArgs& a, int64_t seq, int kvh, int b,
                                              Smem& sm) {
   const int tid = threadIdx.x, lane = tid & 63;
@@ -548,15 +640,15 @@ __device__ __forceinline__ void merge_splits(const DecodeArgs& a, int64_t seq, i
   if (tid == 0) store_agent(ticket, 0ull);
   for (int h = wave; h < G; h += NW) {
     const int64_t bq = (int64_t)b * a.Hq + a.q_head(kvh * G + h);
-    if (Sn <= 4) merge_head<4, DEBUG>(a, bq, lane);
-    else if (Sn <= 8) merge_head<8, DEBUG>(a, bq, lane);
-    else if (Sn <= 16) merge_head<16, DEBUG>(a, bq, lane);
-    else merge_head<kMaxMergedSplits, DEBUG>(a, bq, lane);
+    if (Sn <= 4) merge_head<4, DEBUG, EMPTY>(a, bq, lane);
+    else if (Sn <= 8) merge_head<8, DEBUG, EMPTY>(a, bq, lane);
+    else if (Sn <= 16) merge_head<16, DEBUG, EMPTY>(a, bq, lane);
+    else merge_head<kMaxMergedSplits, DEBUG, EMPTY>(a, bq, lane);
   }
 }
 
 // VF: value format, 0 fp16 values, 1 INT8 values, 2 INT8 values with the
-// power-of-two weights of eq. logsm.
+// power-of-two weights of eq. logsm, 3 values in 4 bits.
 // Value blocks (of two, 16 registers each; INT8 values 8) loaded before the
 // scores; the others are loaded after them, since held meanwhile they would not
 // fit the kernel's registers without spills. CU-wide kernels: 128 registers at
@@ -571,8 +663,8 @@ __device__ __forceinline__ void merge_splits(const DecodeArgs& a, int64_t seq, i
 // -> 6.1).
 template <int MODE, int K, int VF, bool POOL>
 constexpr int kEarlyValueBlocks =
-    POOL ? (MODE == kScorePot ? (K == 2 ? 0 : 1) : MODE == kScoreDs4a ? (K >= 1 ? 0 : 1) : 2)
-    : K == 0            ? 2
+    POOL ? (VF == 3 ? 2 : MODE == kScorePot ? (K == 2 ? 0 : 1) : MODE == kScoreDs4a ? (K >= 1 ? 0 : 1) : 2)
+    : K == 0 || VF == 3 ? 2
     : VF != 0           ? (K == 2 ? 0 : 2)
     : MODE == kScorePot ? (K == 3 ? 2 : K == 2 ? 0 : 1)
                         : 0;
@@ -589,8 +681,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   constexpr bool kPool = NW > kWaves;
   constexpr int kBlk = 64 * NW;
   __shared__ DecodeSmem<MODE, NW> sm;
-  constexpr bool V8 = VF != 0;
+  constexpr int VK = value_kind(VF);
+  constexpr bool V8 = VK == kValI8;
+  constexpr bool V4 = VK == kValI4;
   constexpr bool kPow2 = VF == 2;
+  __shared__ MinimaSums<VK, NW> sz;
 
   const int tid = threadIdx.x, lane = tid & 63;
   // the wave index is uniform in a wave; saying so keeps the tile loop's
@@ -601,8 +696,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   const int64_t row0 = seq * a.t_cap;
   const int8_t* eseq = V8 ? a.v_exp + row0 : nullptr;
   // ---- per-wave streaming over 64-key tiles ------------------------------------
-  const int t_begin = split * a.split_len;
-  const int t_end = min(a.T, t_begin + a.split_len);
+  // With a length per sequence (4-bit values) each is cut into its own n_splits ranges
+  // of whole tiles, of which the last may be empty.
+  int t_all = a.T, split_len = a.split_len;
+  if constexpr (V4) {
+    if (a.seq_lens != nullptr) {
+      t_all = min(max(a.seq_lens[b], 0), a.T);
+      split_len = ((t_all + a.n_splits - 1) / a.n_splits + kWTile - 1) / kWTile * kWTile;
+    }
+  }
+  const int t_begin = split * split_len;
+  const int t_end = min(t_all, t_begin + split_len);
   const int n_tiles = (t_end - t_begin + kWTile - 1) / kWTile;
   const int row = lane & 15, grp = lane >> 4, hrow = row & 7, part = row >> 3;
   const bool hvalid = hrow < G;
@@ -616,12 +720,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // The sequence's new token (fused append) belongs to the workgroup whose
   // range holds row T - 1.
   const bool appends = (MODE == kScorePot || MODE == kScoreDs4a) && a.app_k != nullptr &&
-                       split == a.n_splits - 1;  // uniform per workgroup
+                       (V4 ? t_begin < t_all && t_end == t_all
+                           : split == a.n_splits - 1);  // uniform per workgroup
   int gref = 0;
-  float lsum = 0.0f;  // INT8 values: this lane's sum of the unscaled weights
+  float lsum = 0.0f;  // INT8 and 4-bit values: this lane's sum of the unscaled weights
+  // 4-bit values v = (z + 8 s) + s (n - 8): the matrix cores sum the weights p s times
+  // n - 8, and this lane the p times z + 8 s. The weights have to stay in fp16 range whatever s is: p is
+  // formed with 2^-e_ref, a power of two no smaller than any s so far (fp16 s: e_ref in
+  // [-24, 14]), and e_ref rises like the running maximum does. step_top: 2^e_ref as
+  // fp16, twice.
+  float zsum = 0.0f;
+  int e_ref = -24;
+  uint32_t step_top = 0x00010001u;
+  NibbleConst nib{0x000F000Fu, 0x00F000F0u, 0x64006400u};
+  if constexpr (V4) asm("" : "+v"(nib.even), "+v"(nib.odd), "+v"(nib.exp));
 
   // acc[4], fp16 values: the sums of the weights, as one more column of P.V
-  constexpr int kAcc = V8 ? 4 : 5;
+  constexpr int kAcc = VK != kValF16 ? 4 : 5;
   float4v acc[kAcc];
 #pragma unroll
   for (int nb = 0; nb < kAcc; ++nb) acc[nb] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
@@ -649,7 +764,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   } else {
     st.codes = reinterpret_cast<const uint8_t*>(a.k_f16 + row0 * kDim);
   }
-  if constexpr (V8) {
+  if constexpr (V4) {
+    st.values = a.v4 + row0 * (kI4GroupBytes / 8);
+  } else if constexpr (V8) {
     st.values = a.v8 + row0 * kDim;
     st.exps = reinterpret_cast<const uint8_t*>(a.v_exp + row0);
   } else {
@@ -671,13 +788,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // with short scores slower: PoT-4 decoded to weights 211 us against 200 at
   // B = 64, T = 32768, 34.5 against 33.3 at B = 16, T = 16384.)
   constexpr int kEarlyV = kEarlyValueBlocks<MODE, K, VF, kPool>;
-  ValRegs<V8> vr;
+  ValRegs<VK> vr;
   uint4 ksc[2];
   auto load_tile_scales = [&](int jt) {
     if constexpr (MODE != kScoreFp16) load_scales(st, t_begin + kWTile * jt, lane, ksc);
   };
   auto load_tile_values = [&](int jt) {
-    load_values_buf<V8, 0, kEarlyV>(st, t_begin + kWTile * jt, lane, vr);
+    load_values_buf<VK, 0, kEarlyV>(st, t_begin + kWTile * jt, lane, vr);
   };
   // A wave's first keys and scales are requested at once, unless the tile holds
   // the row that is being appended: then after the barrier below. The first
@@ -706,7 +823,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // The append and the query preparation while the first tiles load; one
   // barrier publishes all of it.
   if constexpr (MODE == kScorePot || MODE == kScoreDs4a) {
-    if (appends) gmin = append_token<K>(a, seq, wave);
+    if (appends) gmin = append_token<K, VK>(a, seq, wave, t_all);
   }
   prepare_queries<MODE, G, K, NW>(a, kvh, b, sm, DEBUG && split == 0, qin);
   if constexpr (V8) {
@@ -757,6 +874,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   float xv[8];
   int m_new = m_run;
   bool first = true;
+  bool step_rises = false;  // 4-bit values: an s of the tile is above 2^e_ref
   auto stage1 = [&](const KeyRegs<MODE, K>& ks, KeyRegs<MODE, K>& knext, int jt) {
     const int t0 = t_begin + kWTile * jt;
     // the next tile's keys (past the range: the last tile again, unused)
@@ -794,7 +912,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
       // keeps the matrix instructions above here (and so their operands' live
       // ranges short): the compiler would sink them to their first use
       asm volatile("" : "+v"(d[0]), "+v"(d[1]));
-      if constexpr (kEarlyV < 2) load_values_buf<V8, kEarlyV, 2>(st, t0, lane, vr);
+      if constexpr (kEarlyV < 2) load_values_buf<VK, kEarlyV, 2>(st, t0, lane, vr);
       // ---- 2. scores to the log2 domain ----
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -821,7 +939,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
       for (int i = 0; i < 8; ++i) xv[i] = (k0 + i < t_end) ? xv[i] : -INFINITY;
       // weights past the range are 0; fp16 value bytes there could be inf or
       // NaN and are cleared, INT8 value bytes are always finite numbers
-      if constexpr (!V8) mask_values(t0, t_end, lane, vr);
+      if constexpr (V4) mask_steps(k0, t_end, vr);
+      else if constexpr (!V8) mask_values(t0, t_end, lane, vr);
+    }
+    if constexpr (V4) {
+      const uint32_t top = max_pairs(max_pairs(vr.s.x, vr.s.y), max_pairs(vr.s.z, vr.s.w));
+      step_rises = max_pairs(top, step_top) != step_top;
     }
 
     // ---- 3. integer running maximum per head ----
@@ -851,11 +974,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // element gets one exact power-of-two product. It runs outside the hot
   // loop below, so the accumulators stay in the matrix-core registers there.
   auto rescale = [&]() {
+    int e_down = 0;
+    if constexpr (V4) {
+      const uint32_t top = max_pairs(max_pairs(vr.s.x, vr.s.y), max_pairs(vr.s.z, vr.s.w));
+      const int bits = wave_max_i32((int)max(top & 0xFFFFu, top >> 16));
+      const float s = __half2float(__ushort_as_half((unsigned short)bits));
+      const int e = max(e_ref, s > 0.0f ? (int)__builtin_amdgcn_frexp_expf(s) : e_ref);
+      e_down = e_ref - e;
+      e_ref = e;
+      // 2^e as fp16: subnormal below 2^-14
+      step_top = (e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24)) * 0x00010001u;
+    }
     if (first) {  // nothing is summed yet
       m_run = m_new;
       return;
     }
-    const float f = (m_run == INT_MIN) ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, m_run - m_new);
+    const float f =
+        (m_run == INT_MIN) ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, m_run - m_new + e_down);
     const int arow = lane & 15, acol = lane >> 4;
 #pragma unroll
     for (int nb = 0; nb < kAcc; ++nb) {
@@ -866,7 +1001,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
                                                  0, 0, 0);
       acc[nb] = d;
     }
-    if constexpr (V8) lsum *= f;
+    if constexpr (V8 || V4) lsum *= f;
+    if constexpr (V4) zsum *= f;
     m_run = m_new;
   };
 
@@ -878,11 +1014,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     // rows 0-7 = hi, 8-15 = lo of the part-0 weights; block kb = 1 takes rows
     // 0-7 = lo, 8-15 = hi of the part-1 weights. Rows h and h + 8 are summed
     // at the end, so both blocks see hi + lo of every weight.
-    const float bias = hvalid ? kPScale - (float)m_run : 0.0f;
+    const float bias = hvalid ? (V4 ? kPScale - (float)e_ref : kPScale) - (float)m_run : 0.0f;
     uint32_t hw[4], lw[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float p0, p1;
+      // the two keys of an operand dword; 4-bit values have 0 2, 1 3, 4 6, 5 7
+      const int k0 = V4 ? (i & 1) + 4 * (i >> 1) : 2 * i, k1 = V4 ? k0 + 2 : k0 + 1;
       if constexpr (kPow2) {
         // A~ = 2^-k with k = M - ceil(x - 1/2) (M - x rounded half up):
         // p = 2^(ceil(x - 1/2) - M + 12), exact; keys masked to -inf get 0.
@@ -899,8 +1037,20 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
         p0 = pw(xv[2 * i]);
         p1 = pw(xv[2 * i + 1]);
       } else {
-        p0 = __builtin_amdgcn_exp2f(xv[2 * i] + bias);
-        p1 = __builtin_amdgcn_exp2f(xv[2 * i + 1] + bias);
+        p0 = __builtin_amdgcn_exp2f(xv[k0] + bias);
+        p1 = __builtin_amdgcn_exp2f(xv[k1] + bias);
+      }
+      if constexpr (V4) {
+        const uint32_t sw[4] = {vr.s.x, vr.s.y, vr.s.z, vr.s.w};
+        const uint32_t zw[4] = {vr.z.x, vr.z.y, vr.z.z, vr.z.w};
+        const half2v s0 = __builtin_bit_cast(half2v, sw[k0 / 2]), s1 = __builtin_bit_cast(half2v, sw[k1 / 2]);
+        const half2v z0 = __builtin_bit_cast(half2v, zw[k0 / 2]), z1 = __builtin_bit_cast(half2v, zw[k1 / 2]);
+        lsum += p0;
+        lsum += p1;
+        zsum = __builtin_fmaf(p0, __builtin_fmaf((float)s0[k0 & 1], 8.0f, (float)z0[k0 & 1]), zsum);
+        zsum = __builtin_fmaf(p1, __builtin_fmaf((float)s1[k1 & 1], 8.0f, (float)z1[k1 & 1]), zsum);
+        p0 = __fmul_rn(p0, (float)s0[k0 & 1]);
+        p1 = __fmul_rn(p1, (float)s1[k1 & 1]);
       }
       if constexpr (V8) {
         // the softmax sum takes p; A.V takes p 2^(g_ref - g) (exact scaling)
@@ -927,11 +1077,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     const half8 af0 = __builtin_bit_cast(half8, make_uint4(a0w[0], a0w[1], a0w[2], a0w[3]));
     const half8 af1 = __builtin_bit_cast(half8, make_uint4(a1w[0], a1w[1], a1w[2], a1w[3]));
     auto bfrag = [&](int kb, int nb) -> half8 {
-      if constexpr (V8) return int8_value_fragment(vr.f[kb][nb]);
+      if constexpr (V4) {
+        const uint4 w = vr.f[kb];
+        return nb & 1 ? int4_value_fragment<true>(nb < 2 ? w.x : w.z, nb < 2 ? w.y : w.w, nib)
+                      : int4_value_fragment<false>(nb < 2 ? w.x : w.z, nb < 2 ? w.y : w.w, nib);
+      } else if constexpr (V8) return int8_value_fragment(vr.f[kb][nb]);
       else return __builtin_bit_cast(half8, vr.f[kb][nb]);
     };
     auto weight_sums = [&]() {
-      if constexpr (!V8) {
+      if constexpr (VK == kValF16) {
         half8 ones;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.0f;
@@ -977,7 +1131,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
 #pragma nounroll
     for (;;) {
       stage1(kr[0], kr[1], j);
-      if (__any(m_new != m_run)) break;
+      if (__any(m_new != m_run || step_rises)) break;
       stage2();
       advance();
       if (j >= n_tiles) break;
@@ -1005,8 +1159,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
         if (lane < 32) sm.wo[wave][4 * grp + r][16 * nb + row] = sum;
       }
   }
+  // 4-bit values: the sums' reference is 2^(m_run + e_ref) (in range: a score beyond
+  // 2^31 has saturated)
+  if constexpr (V4) {
+    if (m_run != INT_MIN) m_run = min(max(m_run, INT_MIN + 64), INT_MAX - 64) + e_ref;
+  }
   if (lane < 8) sm.wm[wave][lane] = m_run;
-  if constexpr (V8) {
+  if constexpr (V4) {
+    zsum += dpp_move<kDppRowRor8>(zsum);
+    const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(zsum), __float_as_uint(zsum),
+                                                      false, false);
+    zsum = __uint_as_float(r16[0]) + __uint_as_float(r16[1]);
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(zsum), __float_as_uint(zsum),
+                                                      false, false);
+    zsum = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
+    if (lane < 8) sz.z[wave][lane] = zsum;
+  }
+  if constexpr (V8 || V4) {
     // sum of the weights over the 8 lanes that formed a head's
     lsum += dpp_move<kDppRowRor8>(lsum);
     const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(lsum), __float_as_uint(lsum),
@@ -1048,8 +1217,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
                  sm.wo[i][h][d], o);
     }
     if constexpr (V8) o = __builtin_amdgcn_ldexpf(o, -gref);
+    if constexpr (V4) o += wave_sum(f_w * (lane < NW ? sz.z[lane < NW ? lane : 0][h] : 0.0f));
     if (Sn == 1) {
-      a.out[bq * kDim + d] = o / l;
+      a.out[bq * kDim + d] = quotient(o, l, V4);
       if constexpr (DEBUG) {
         if (d == 0 && a.dbg_m_final) a.dbg_m_final[bq] = M;
         if (d == 0 && a.dbg_m_split) a.dbg_m_split[bq] = M;
@@ -1077,7 +1247,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     }
   }
   if constexpr (kPool)
-    if (Sn > 1 && a.ticket != 0) merge_splits<G, DEBUG, NW>(a, seq, kvh, b, sm);
+    if (Sn > 1 && a.ticket != 0) merge_splits<G, DEBUG, V4, NW>(a, seq, kvh, b, sm);
 }
 
 // Merges the key splits of one (batch, query head): M = max_s M_s and
@@ -1088,7 +1258,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
 // memory latency for the whole merge); more splits go through a loop.
 constexpr int kCombineWaves = 4;
 constexpr int kCombineBatch = 16;  // splits per wave in the single-batch path
-template <bool DEBUG>
+// EMPTY: splits without keys have M_s = INT_MIN and sums of 0 (a sequence without any: O = 0).
+template <bool DEBUG, bool EMPTY>
 __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const DecodeArgs a) {
   __shared__ float so[kCombineWaves][kDim];
   __shared__ float sl[kCombineWaves];
@@ -1121,7 +1292,8 @@ __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const Decod
     if (d == 0) smax[w] = mw;
     __syncthreads();
     M = max(max(smax[0], smax[1]), max(smax[2], smax[3]));
-    const float f_l = valid ? __builtin_amdgcn_ldexpf(1.0f, m_l - M) : 0.0f;
+    const float f_l = valid && !(EMPTY && m_l == INT_MIN)
+                          ? __builtin_amdgcn_ldexpf(1.0f, m_l - M) : 0.0f;
     float fl = f_l * l_l;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) fl += __shfl_xor(fl, o, 64);
@@ -1142,7 +1314,7 @@ __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const Decod
     M = max(max(smax[0], smax[1]), max(smax[2], smax[3]));
 #pragma unroll 8
     for (int s = w; s < Sn; s += kCombineWaves) {
-      const float f = __builtin_amdgcn_ldexpf(1.0f, pm[s] - M);
+      const float f = EMPTY && pm[s] == INT_MIN ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, pm[s] - M);
       L = fmaf(f, pl[s], L);
       O = fmaf(f, po[s * kDim + d], O);
     }
@@ -1158,7 +1330,7 @@ __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const Decod
       O += so[i][d];
       L += sl[i];
     }
-    a.out[bq * kDim + d] = O / L;
+    a.out[bq * kDim + d] = quotient(O, L, EMPTY);
     if constexpr (DEBUG) {
       if (d == 0 && a.dbg_m_final) a.dbg_m_final[bq] = M;
     }
@@ -1189,7 +1361,7 @@ static hipError_t launch_t(const DecodeArgs& a, hipStream_t stream, hipEvent_t e
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (ev_end != nullptr && (e = hipEventRecord(ev_end, stream)) != hipSuccess) return e;
   if (a.n_splits == 1 || a.ticket != 0) return hipSuccess;
-  hipLaunchKernelGGL((combine_kernel<DEBUG>), dim3((uint32_t)(a.B * a.Hq)),
+  hipLaunchKernelGGL((combine_kernel<DEBUG, VF == 3>), dim3((uint32_t)(a.B * a.Hq)),
                      dim3(64 * kCombineWaves), 0, stream, a);
   return hipGetLastError();
   }
@@ -1230,7 +1402,7 @@ static hipError_t launch_g(int G, int mant_bits, const DecodeArgs& a, hipStream_
 template <int MODE, int VF>
 hipError_t launch_mode_vf(int G, int mant_bits, bool debug, const DecodeArgs& a,
                           hipStream_t stream, hipEvent_t e0, hipEvent_t e1) {
-  if constexpr (MODE == kScoreFp16)
+  if constexpr (MODE == kScoreFp16 || VF == 3)  // formats without taps
     return launch_g<MODE, false, VF>(G, mant_bits, a, stream, e0, e1);
   else
     return debug ? launch_g<MODE, true, VF>(G, mant_bits, a, stream, e0, e1)

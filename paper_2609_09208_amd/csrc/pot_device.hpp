@@ -249,4 +249,49 @@ __device__ __forceinline__ int store_value_token_i8_wave(const uint16_t* __restr
   return g;
 }
 
+// 4-bit values: groups of 8 tokens, kI4GroupBytes bytes each. Byte 16 (d % 16) +
+// 8 (d / 32) + t % 8 of a group has the n of dimension d in its low half where
+// d % 32 < 16 and in its high half elsewhere, so 16 consecutive bytes are the
+// matrix-core operands of 8 tokens for the dimensions c, 16 + c, 32 + c and 48 + c,
+// and a token has its bytes to itself; behind them the tokens' 8 fp16 steps s and 8
+// fp16 minima z. A value is z + s n.
+constexpr int kI4Steps = 256, kI4Minima = 272, kI4GroupBytes = 288;
+
+// The row's step: the smallest fp16 number >= fl(fl(max - min) / 15), as bits.
+// lo and hi are fp16 numbers, so the range is at most 131008 and s at most 8736.
+__device__ __forceinline__ uint16_t value_step_i4(float lo, float hi) {
+  const float f = (hi - lo) / 15.0f;  // correctly rounded
+  const uint16_t b = __half_as_ushort(__float2half_rn(f));
+  return __half2float(__ushort_as_half(b)) < f ? b + 1 : b;
+}
+// An element as the 4-bit store sees it: infinities are the largest finite numbers.
+__device__ __forceinline__ float value_in_i4(float v) {
+  return v != v ? v : __builtin_amdgcn_fmed3f(v, -65504.0f, 65504.0f);
+}
+// n = min(15, rne(fl(fl(v - z) * inv))), inv = fl(1 / s) (0 for s = 0); 0 for NaN.
+__device__ __forceinline__ uint32_t value_code_i4(float v, float z, float inv) {
+  const float n = rintf(__fmul_rn(v - z, inv));
+  return n > 0.0f ? (uint32_t)fminf(n, 15.0f) : 0u;
+}
+// One token, quantised and stored by the calling wave (lane = dim). NaN elements are
+// passed over by the minimum and the maximum (a row of NaNs: z = s = 0).
+__device__ __forceinline__ void store_value_token_i4_wave(const uint16_t* __restrict__ v_row,
+                                                          uint8_t* __restrict__ v_seq,
+                                                          int64_t t) {
+  const int lane = lane_id();
+  const float v = value_in_i4(__half2float(__ushort_as_half(v_row[lane])));
+  const float hi = wave_max(v), lo = -wave_max(-v);
+  const bool any = hi == hi;
+  const uint16_t step = any ? value_step_i4(lo, hi) : 0;
+  const uint16_t zero = any ? __half_as_ushort(__float2half_rn(lo)) : 0;
+  const float s = __half2float(__ushort_as_half(step));
+  const uint32_t n = value_code_i4(v, __half2float(__ushort_as_half(zero)), s > 0.0f ? 1.0f / s : 0.0f);
+  uint8_t* g = v_seq + (t / 8) * kI4GroupBytes;
+  // lanes d and d + 16 (d % 32 < 16) share a byte
+  const auto r = __builtin_amdgcn_permlane16_swap(n, n, false, false);
+  if ((lane & 16) == 0) g[16 * (lane & 15) + 8 * (lane >> 5) + t % 8] = (uint8_t)(r[0] | (r[1] << 4));
+  if (lane == 0) *reinterpret_cast<uint16_t*>(g + kI4Steps + 2 * (t % 8)) = step;
+  if (lane == 1) *reinterpret_cast<uint16_t*>(g + kI4Minima + 2 * (t % 8)) = zero;
+}
+
 }  // namespace potattn

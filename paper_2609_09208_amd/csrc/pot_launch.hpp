@@ -109,6 +109,10 @@ struct DecodeArgs {
   int32_t claim_tiles;         // CU-wide workgroups: tiles from a counter, else in fixed order
   int32_t wg_waves;            // waves per decode workgroup: 4, or pool_waves(...)
   uint32_t q_of_kv[kMaxHqArg / 4];  // [Hkv][G] query heads served by each kv head, a byte each
+  // 4-bit values
+  const uint8_t* v4;           // value cache, kI4GroupBytes per 8 tokens
+  uint8_t* app_v4;             // the same cache, written at the appended row only
+  const int32_t* seq_lens;     // [B] keys of each sequence (clamped to 0 .. T), NULL: T for all
 
   // Query head g of a group in [Hkv][G] order (kvh * G + g).
   __host__ __device__ int q_head(int i) const { return (q_of_kv[i >> 2] >> (8 * (i & 3))) & 0xFF; }
@@ -124,7 +128,7 @@ struct DecodeArgs {
 // waves, 64 units 86.2 and 85.8, 4 units 13.2 and 12.3).
 constexpr int pool_waves(int mode, int mant_bits, int vf) {
   return mode == kScorePot    ? (mant_bits <= 2 ? 16 : 12)
-         : mode == kScoreDs4a ? ((mant_bits > 0 || vf == 1) ? 16 : 12)
+         : mode == kScoreDs4a ? ((mant_bits > 0 || vf == 1 || vf == 3) ? 16 : 12)
          : mode == kScoreInt8 ? 12
                               : 0;
 }
@@ -141,8 +145,8 @@ constexpr int kMaxKeys = (1 << 24) - 8;
 constexpr int query_words(int G) { return (33 * G + 63) / 64 * 64; }
 
 // vf: value format. 0: fp16 value cache (a.v); 1: INT8 value cache (a.v8,
-// a.v_exp); 2: INT8 values with the power-of-two weights of eq. logsm.
-// Formats 1 and 2 exist for the score modes kScorePot and kScoreDs4a only.
+// a.v_exp); 2: INT8 values with the power-of-two weights of eq. logsm; 3: values
+// in 4 bits (a.v4, a.seq_lens; no debug taps). Formats 1 to 3 exist for the score modes kScorePot and kScoreDs4a only.
 // ev_begin / ev_end (may be null) are recorded on the stream right before and
 // right after the decode kernel.
 hipError_t launch_decode(int mode, int G, int mant_bits, bool debug, int vf,
@@ -154,5 +158,39 @@ hipError_t launch_decode(int mode, int G, int mant_bits, bool debug, int vf,
 template <int MODE, int VF>
 hipError_t launch_mode_vf(int G, int mant_bits, bool debug, const DecodeArgs& a,
                           hipStream_t stream, hipEvent_t e0, hipEvent_t e1);
+
+// 4-bit values, one step and minimum per token (pot_device.hpp).
+hipError_t launch_store_values_i4(const uint16_t* src, int64_t n_seq, int64_t n_tok,
+                                  int64_t t_cap, int64_t t0, uint8_t* v_u4, hipStream_t stream);
+
+// Rows t0 .. t0 + n_tok - 1 of every sequence of a cache as dense fp16 rows.
+hipError_t launch_load_keys(int mant_bits, int hadamard, const uint8_t* codes_se,
+                            const uint8_t* codes_m, const float* key_scale, int64_t n_seq,
+                            int64_t n_tok, int64_t t_cap, int64_t t0, uint16_t* k,
+                            hipStream_t stream);
+// fmt: 0 fp16 values, 1 INT8 (v_exp: their exponents), 2 4-bit.
+hipError_t launch_load_values(int fmt, const void* cache, const int8_t* v_exp, int64_t n_seq,
+                              int64_t n_tok, int64_t t_cap, int64_t t0, uint16_t* v,
+                              hipStream_t stream);
+
+// Norm and rotation of a projection's rows. dtype: pot_dtype.
+struct RowsIn {
+  const void* data;
+  int64_t stride_b, stride_s, stride_h;  // elements
+};
+struct NormRopeArgs {
+  RowsIn q, k, v;               // data NULL: left out
+  const void *q_weight, *k_weight;  // NULL: no norm
+  const int64_t* positions;     // [n_axes][B][S]
+  const double* inv_freq;       // [rot_dim / 2]
+  void* q_out;                  // [B][Hq][S][64]
+  uint16_t *k_out, *v_out;      // fp16 [B][Hkv][S][64]
+  float eps;
+  int32_t B, S, Hq, Hkv;
+  int32_t dtype, weight_dtype, q_out_dtype;
+  int32_t rot_dim, neighbours;
+  uint8_t axis_of_pair[32];
+};
+hipError_t launch_norm_rope(const NormRopeArgs& a, hipStream_t stream);
 
 }  // namespace potattn
