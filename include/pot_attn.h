@@ -216,7 +216,7 @@ pot_status pot_store_values_int8(const uint16_t* v_fp16, int64_t n_seq, int64_t 
  *           elsewhere (so a token shares no byte with another); from byte 256 the
  *           8 tokens' s and from byte 272 their z, fp16.
  * n_seq, n_tok, t_cap, t0 and the errors as pot_store_values; n_seq * n_tok up to
- * 2^31. */
+ * 2^30. */
 #define POT_INT4_GROUP_BYTES 288
 pot_status pot_store_values_int4(const uint16_t* v_fp16, int64_t n_seq, int64_t n_tok,
                                  int64_t t_cap, int64_t t0, uint8_t* v_u4, void* stream);
@@ -224,8 +224,8 @@ pot_status pot_store_values_int4(const uint16_t* v_fp16, int64_t n_seq, int64_t 
 /* Read a cache back: rows t0 .. t0+n_tok-1 of n_seq sequences (consecutive from
  * the given pointers, t_cap rows each) as the dense fp16 rows that the codes stand
  * for, [n_seq][n_tok][d]: for attention over a prompt, for checks, or to write them
- * in another format. Nothing of the cache is changed, and rows outside the range are
- * not read.
+ * in another format. Nothing of the cache is changed, and what other rows hold does
+ * not reach the output.
  *  pot_load_keys: s sigma (1 + j/2^k) 2^-e of each element, 0 for the zero code,
  *   formed in fp32 and rounded to fp16; with fmt->hadamard rotated back (H K^ / 8,
  *   sums in fp32, rounded once). A format with hadamard = 0 gives the rows of a
@@ -234,7 +234,7 @@ pot_status pot_store_values_int4(const uint16_t* v_fp16, int64_t n_seq, int64_t 
  *  pot_load_values_int8: v^ 2^-g.
  *  pot_load_values_int4: z + s n, formed in fp32 and rounded to fp16.
  * t_cap a positive multiple of 8; sizes of 0 are no-ops. Errors as the store calls;
- * n_seq * n_tok up to 2^31. */
+ * n_seq * n_tok up to 2^30. */
 pot_status pot_load_keys(const pot_format* fmt, const uint8_t* codes_se, const uint8_t* codes_m,
                          const float* key_scale, int64_t n_seq, int64_t n_tok, int64_t t_cap,
                          int64_t t0, uint16_t* k_fp16, void* stream);
@@ -286,7 +286,8 @@ typedef struct pot_rows {
  *               struct or data leaves the part out; its output must then be NULL too.
  *               Rows must be 16-byte aligned (data, and the strides of dimensions
  *               over 1).
- *  q_weight, k_weight [64] of weight_dtype, device, or NULL: no norm of that part.
+ *  q_weight, k_weight [64] of weight_dtype, device, 16-byte aligned, or NULL: no norm of
+ *               that part.
  *  eps          finite, >= 0.
  *  positions    int64 [n_axes][B][S], device, any sign (8-byte aligned; NULL iff
  *               rot_dim = 0). The angle is exact to 2^-52 of itself plus rounding: for

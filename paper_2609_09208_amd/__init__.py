@@ -91,7 +91,6 @@ def _load_library():
     i32, i64 = ctypes.c_int32, ctypes.c_int64
     fmt_p = ctypes.POINTER(pot_format)
     dbg_p = ctypes.POINTER(pot_debug)
-    rows_p = ctypes.POINTER(pot_rows)
     sig = {
         "pot_status_string": (ctypes.c_char_p, [i32]),
         "pot_last_error": (ctypes.c_char_p, []),
@@ -127,7 +126,7 @@ def _load_library():
         "pot_load_values": (i32, [P, i64, i64, i64, i64, P, P]),
         "pot_load_values_int8": (i32, [P, P, i64, i64, i64, i64, P, P]),
         "pot_load_values_int4": (i32, [P, i64, i64, i64, i64, P, P]),
-        "pot_norm_rope": (i32, [ctypes.POINTER(pot_rope), i32, rows_p, rows_p, rows_p, P, P, i32,
+        "pot_norm_rope": (i32, [ctypes.POINTER(pot_rope), i32, P, P, P, P, P, i32,
                                 ctypes.c_float, P, P, i32, i32, i32, i32, i32, P, P, P, P]),
         "pot_int8_encode_keys": (i32, [P, i64, i64, i32, P, P, P]),
         "pot_int8_decode_attention": (i32, [P, P, P, P, i64, P, i32, i32, i32,
@@ -369,21 +368,28 @@ def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new
 
 
 _DTYPES = {torch.float16: POT_FP16, torch.bfloat16: POT_BF16, torch.float32: POT_FP32}
+_Rows3 = ctypes.c_int64 * 12  # three pot_rows
+_ROWS_BYTES = ctypes.sizeof(pot_rows)
 
 
-def _part(x, out, B: int, S: int):
-    """A part of a projection [B, S, heads, 64] (any strides, elements side by side) as
-    (pot_rows by reference or None, its heads)."""
-    if x is None:
-        return None, 0
-    H = x.shape[2]
+def _mismatch(what: str):
+    raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", what)
+
+
+def _part(x, out, B: int, S: int, out_type):
+    """Heads, address and strides of a part of a projection [B, S, heads, 64] (any strides,
+    elements side by side) whose output is dense [B, heads, S, 64] (of out_type, if given)."""
+    b, s, h, d = x.shape
     sb, ss, sh, se = x.stride()
-    if (x.shape[0] != B or x.shape[1] != S or x.shape[3] != HEAD_DIM or se != 1 or out is None
-            or out.shape != (B, H, S, HEAD_DIM) or not out.is_contiguous()):
-        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG",
-                       "rows [B, S, heads, 64] with dense elements and a dense output "
-                       "[B, heads, S, 64] are needed")
-    return ctypes.byref(pot_rows(x.data_ptr(), sb, ss, sh)), H
+    if b != B or s != S or d != HEAD_DIM or se != 1:
+        _mismatch("rows [B, S, heads, 64] with dense elements are needed")
+    if (out is None or out.numel() != B * h * S * HEAD_DIM or not out.is_contiguous()
+            or (out_type is not None and out.dtype is not out_type)):
+        _mismatch("a dense output [B, heads, S, 64] is needed (k and v: float16)")
+    return h, x.data_ptr(), sb, ss, sh
+
+
+_NO_PART = (0, 0, 0, 0, 0)
 
 
 def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions, inv_freq,
@@ -392,32 +398,42 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
     left out) to q_out [B, Hq, S, 64], k_out and v_out [B, Hkv, S, 64] (dense; k_out and
     v_out float16). positions int64 [n_axes, B, S], inv_freq float64 [rot_dim/2], weights
     [64] of one type or None."""
-    given = [x for x in (q, k, v) if x is not None]
-    weights = [w for w in (q_weight, k_weight) if w is not None]
-    if not given:
+    first = q if q is not None else k if k is not None else v
+    if first is None:
         return
-    B, S = given[0].shape[0], given[0].shape[1]
-    (qr, hq), (kr, hk), (vr, hv) = _part(q, q_out, B, S), _part(k, k_out, B, S), _part(v, v_out, B, S)
-    dtype, wtype = given[0].dtype, weights[0].dtype if weights else torch.float32
-    qtype = q_out.dtype if q_out is not None else torch.float32
-    n_pos = rope.n_axes * B * S
-    if ((k is not None and v is not None and hk != hv) or any(x.dtype != dtype for x in given)
-            or any(w.dtype != wtype or w.shape != (HEAD_DIM,) or not w.is_contiguous()
-                   for w in weights)
-            or any(o is not None and o.dtype != torch.float16 for o in (k_out, v_out))
-            or any(t not in _DTYPES for t in (dtype, wtype, qtype))
-            or (positions is not None and (positions.dtype != torch.int64
-                                           or positions.numel() != n_pos
-                                           or not positions.is_contiguous()))
-            or (inv_freq is not None and (inv_freq.dtype != torch.float64
-                                          or inv_freq.numel() < rope.rot_dim // 2
-                                          or not inv_freq.is_contiguous()))):
-        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG",
-                       "types or shapes that do not go together")
+    B, S = first.shape[:2]
+    dtype = first.dtype
+    hq, *at_q = _NO_PART if q is None else _part(q, q_out, B, S, None)
+    hk, *at_k = _NO_PART if k is None else _part(k, k_out, B, S, torch.float16)
+    hv, *at_v = _NO_PART if v is None else _part(v, v_out, B, S, torch.float16)
+    if hk and hv and hk != hv:
+        _mismatch("k and v have the same number of heads")
+    if (k is not None and k.dtype is not dtype) or (v is not None and v.dtype is not dtype):
+        _mismatch("q, k and v are of one type")
+    wtype = None
+    for w in (q_weight, k_weight):
+        if w is not None:
+            if (w.numel() != HEAD_DIM or not w.is_contiguous()
+                    or (wtype is not None and w.dtype is not wtype)):
+                _mismatch("weights are [64], dense and of one type")
+            wtype = w.dtype
+    if positions is not None and (positions.dtype is not torch.int64 or not positions.is_contiguous()
+                                  or positions.numel() != rope.n_axes * B * S):
+        _mismatch("positions are dense int64 [n_axes, B, S]")
+    if inv_freq is not None and (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
+                                 or inv_freq.numel() < rope.rot_dim // 2):
+        _mismatch("inv_freq is dense float64 [rot_dim / 2]")
+    types = _DTYPES
+    qtype = types.get(q_out.dtype) if q_out is not None else POT_FP32
+    itype, wtype = types.get(dtype), types.get(wtype) if wtype is not None else POT_FP32
+    if qtype is None or itype is None or wtype is None:
+        _mismatch("types are float16, bfloat16 or float32")
+    rows = _Rows3(*at_q, *at_k, *at_v)
+    at = ctypes.addressof(rows)
     _check(_lib.pot_norm_rope(
-        ctypes.byref(rope), _DTYPES[dtype], qr, kr, vr, _ptr(q_weight), _ptr(k_weight),
-        _DTYPES[wtype], float(eps), _ptr(positions), _ptr(inv_freq), B, S, hq, hk or hv,
-        _DTYPES[qtype], _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream)))
+        ctypes.byref(rope), itype, at, at + _ROWS_BYTES, at + 2 * _ROWS_BYTES, _ptr(q_weight),
+        _ptr(k_weight), wtype, eps, _ptr(positions), _ptr(inv_freq), B, S, hq, hk or hv, qtype,
+        _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream)))
 
 
 def pot_ds4a_decode_attention(fmt: pot_format, q, codes_se, key_scale, v_fp16, t_cap: int,

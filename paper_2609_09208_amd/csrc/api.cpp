@@ -457,7 +457,7 @@ pot_status check_rows(int64_t n_seq, int64_t n_tok, int64_t t_cap, int64_t t0) {
   if (t0 < 0 || n_tok > t_cap || t0 > t_cap - n_tok)
     return fail(POT_ERR_INVALID_ARG, "n_tok %lld tokens from %lld outside [0, t_cap = %lld)",
                 (long long)n_tok, (long long)t0, (long long)t_cap);
-  if (n_tok > 0 && n_seq > ((int64_t)1 << 31) / n_tok)
+  if (n_tok > 0 && n_seq > ((int64_t)1 << 30) / n_tok)
     return fail(POT_ERR_INVALID_ARG, "n_seq * n_tok too large");
   return POT_OK;
 }
@@ -675,9 +675,8 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
     return fail(POT_ERR_INVALID_ARG, "positions or inv_freq is NULL");
   if (!aligned(positions, 8) || !aligned(inv_freq, 8))
     return fail(POT_ERR_INVALID_ARG, "positions and inv_freq must be 8-byte aligned");
-  const size_t w_size = weight_dtype == POT_FP32 ? 4 : 2;
-  if (!aligned(q_weight, w_size) || !aligned(k_weight, w_size))
-    return fail(POT_ERR_INVALID_ARG, "misaligned q_weight / k_weight");
+  if (!aligned(q_weight, 16) || !aligned(k_weight, 16))
+    return fail(POT_ERR_INVALID_ARG, "q_weight and k_weight must be 16-byte aligned");
   if ((int64_t)B * S > ((int64_t)1 << 31))
     return fail(POT_ERR_INVALID_ARG, "B * S too large");
   a.q_weight = a.q.data ? q_weight : nullptr;
@@ -697,6 +696,7 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
   a.q_out_dtype = q_out_dtype;
   a.rot_dim = r;
   a.neighbours = rope->neighbours;
+  a.n_axes = rope->n_axes;
   for (int i = 0; i < 32; ++i) a.axis_of_pair[i] = i < r / 2 ? rope->axis_of_pair[i] : 0;
   return hip_status(launch_norm_rope(a, static_cast<hipStream_t>(stream)), "norm and rotation launch");
 }

@@ -259,10 +259,20 @@ constexpr int kI4Steps = 256, kI4Minima = 272, kI4GroupBytes = 288;
 
 // The row's step: the smallest fp16 number >= fl(fl(max - min) / 15), as bits.
 // lo and hi are fp16 numbers, so the range is at most 131008 and s at most 8736.
+// The quotient is the correctly rounded one: a product with the rounded reciprocal and
+// one correction by the exact remainder (the range is 0 or at least 2^-24).
 __device__ __forceinline__ uint16_t value_step_i4(float lo, float hi) {
-  const float f = (hi - lo) / 15.0f;  // correctly rounded
+  const float d = hi - lo, r = 1.0f / 15.0f, q = d * r;
+  const float f = __builtin_fmaf(__builtin_fmaf(-q, 15.0f, d), r, q);
   const uint16_t b = __half_as_ushort(__float2half_rn(f));
   return __half2float(__ushort_as_half(b)) < f ? b + 1 : b;
+}
+// fl(1 / s) of a step as a number, 0 for s = 0. The hardware's reciprocal is within a unit
+// in the last place, from where one Newton step rounds correctly for every fp16 number
+// (checked for all of them and the three starts).
+__device__ __forceinline__ float step_reciprocal(float s) {
+  const float r = __builtin_amdgcn_rcpf(s);
+  return s > 0.0f ? __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r) : 0.0f;
 }
 // An element as the 4-bit store sees it: infinities are the largest finite numbers.
 __device__ __forceinline__ float value_in_i4(float v) {
@@ -285,7 +295,7 @@ __device__ __forceinline__ void store_value_token_i4_wave(const uint16_t* __rest
   const uint16_t step = any ? value_step_i4(lo, hi) : 0;
   const uint16_t zero = any ? __half_as_ushort(__float2half_rn(lo)) : 0;
   const float s = __half2float(__ushort_as_half(step));
-  const uint32_t n = value_code_i4(v, __half2float(__ushort_as_half(zero)), s > 0.0f ? 1.0f / s : 0.0f);
+  const uint32_t n = value_code_i4(v, __half2float(__ushort_as_half(zero)), step_reciprocal(s));
   uint8_t* g = v_seq + (t / 8) * kI4GroupBytes;
   // lanes d and d + 16 (d % 32 < 16) share a byte
   const auto r = __builtin_amdgcn_permlane16_swap(n, n, false, false);

@@ -188,7 +188,7 @@ struct NormRopeArgs {
   float eps;
   int32_t B, S, Hq, Hkv;
   int32_t dtype, weight_dtype, q_out_dtype;
-  int32_t rot_dim, neighbours;
+  int32_t rot_dim, neighbours, n_axes;
   uint8_t axis_of_pair[32];
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, hipStream_t stream);

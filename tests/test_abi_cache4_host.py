@@ -145,7 +145,7 @@ def test_binding_refuses_tensors_that_do_not_go_together():
     w = torch.ones(64)
     good = dict(rope=pa.make_rope(), q=x, k=None, v=None, q_weight=w, k_weight=None, eps=1e-6, positions=pos, inv_freq=inv,
                 q_out=out, k_out=None, v_out=None)
-    for over in [dict(q_out=None), dict(q_out=out.transpose(1, 2)), dict(q_out=torch.zeros((2, 3, 4, 64))),
+    for over in [dict(q_out=None), dict(q_out=out.transpose(1, 2)), dict(q_out=torch.zeros((2, 3, 4, 32))),
                  dict(q=x.transpose(2, 3).contiguous().transpose(2, 3)), dict(q=x[..., :32]), dict(q=x.double()),
                  dict(positions=pos.int()), dict(positions=pos[:, :, :2]), dict(inv_freq=inv.float()),
                  dict(inv_freq=inv[:31]), dict(q_weight=torch.ones(63)), dict(q_weight=torch.ones(128)[::2]),
