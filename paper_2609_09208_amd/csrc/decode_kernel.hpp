@@ -56,6 +56,7 @@
 namespace potattn {
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = kBlock / 64;  // waves per workgroup of the default variant
@@ -71,6 +72,9 @@ template <int MODE, int K, int VF>
 constexpr int kPoolWaves = pool_waves(MODE, K, VF);
 constexpr int kWTile = 64;    // keys per wave tile
 constexpr float kPScale = 12.0f;  // p is formed as 2^(x - M + 12) (fp16-normal range)
+// 4-bit values: weights are formed as 2^(x - R + 8) s and may grow to 2^16 (fp16's range) before
+// the reference R rises.
+constexpr float kPScale4 = 8.0f, kMostWeight4 = 65000.0f;
 constexpr int kDppRowRor8 = 0x128;  // DPP row_ror:8: lane l reads lane l ^ 8 within its row of 16
 
 // max(a, b) for scores (never NaN) as v_max_f32 without operand canonicalisation
@@ -402,6 +406,13 @@ __device__ __forceinline__ void mask_values(int t0, int t_end, int lane, ValRegs
   }
 }
 
+// Steps of 0 (constant rows, and keys past the range) as 2^-24, fp16's smallest number.
+__device__ __forceinline__ void least_steps(ValRegs<kValI4>& v) {
+  const uint32_t least = 0x00010001u;
+  v.s = make_uint4(max_pairs(v.s.x, least), max_pairs(v.s.y, least), max_pairs(v.s.z, least),
+                   max_pairs(v.s.w, least));
+}
+
 // Sums of the weights times the values' minima, per wave and head (4-bit values).
 template <int VK, int NW>
 struct MinimaSums {};
@@ -725,13 +736,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   int gref = 0;
   float lsum = 0.0f;  // INT8 and 4-bit values: this lane's sum of the unscaled weights
   // 4-bit values v = (z + 8 s) + s (n - 8): the matrix cores sum the weights p s times
-  // n - 8, and this lane the p times z + 8 s. The weights have to stay in fp16 range whatever s is: p is
-  // formed with 2^-e_ref, a power of two no smaller than any s so far (fp16 s: e_ref in
-  // [-24, 14]), and e_ref rises like the running maximum does. step_top: 2^e_ref as
-  // fp16, twice.
+  // n - 8, and this lane the p times z + 8 s. m_run is then the reference R of both: an
+  // integer no smaller than x + log2 s of any key when it was set, and raised only when a
+  // weight p s would leave fp16's range: a rise by less than 2^8 needs no rescale, so a
+  // wave rescales about once, after its first tile (following every rise of a maximum,
+  // eight heads rescaled in half of a wave's 32 tiles), and no maximum is taken over the
+  // wave before. s = 0 counts as 2^-24, its smallest other value (all n are 0 then), so a
+  // weight below the range bounds p itself by 2^40.
   float zsum = 0.0f;
-  int e_ref = -24;
-  uint32_t step_top = 0x00010001u;
   NibbleConst nib{0x000F000Fu, 0x00F000F0u, 0x64006400u};
   if constexpr (V4) asm("" : "+v"(nib.even), "+v"(nib.odd), "+v"(nib.exp));
 
@@ -874,7 +886,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   float xv[8];
   int m_new = m_run;
   bool first = true;
-  bool step_rises = false;  // 4-bit values: an s of the tile is above 2^e_ref
+  bool tail_tile = false;
+  float bias4 = hvalid ? kPScale4 - (float)INT_MIN : 0.0f;  // 4-bit values: kPScale4 - R
+  uint32_t hw[4], lw[4];  // the weights' fp16 high and low parts, two keys each
   auto stage1 = [&](const KeyRegs<MODE, K>& ks, KeyRegs<MODE, K>& knext, int jt) {
     const int t0 = t_begin + kWTile * jt;
     // the next tile's keys (past the range: the last tile again, unused)
@@ -900,7 +914,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
           const uint32_t w[4] = {ks.c[i].x, ks.c[i].y, ks.c[i].z, ks.c[i].w};
           uint32_t pl[K > 0 ? K : 1];
           if constexpr (K > 0) plane_bits<MODE, K>(ks, i, pl);
-          if constexpr (MODE == kScorePot) d[i] = score_set<K>(w, pl, m22, qop);
+          if constexpr (V4 && MODE == kScorePot) d[i] = score_set_powers<K>(w, pl, qop);
+          else if constexpr (MODE == kScorePot) d[i] = score_set<K>(w, pl, m22, qop);
           else d[i] = score_set_decoded<K>(w, pl, qop, to_int);
           if constexpr (kReloadQ) asm volatile("" : "+v"(d[i]));
         } else if constexpr (MODE == kScoreInt8) {
@@ -921,6 +936,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
         for (int r = 0; r < 4; ++r) {
           float x = d[i][r];
           if constexpr (MODE != kScoreFp16) x = __fmul_rn(x, __uint_as_float(sc[r]));
+          if constexpr (V4) {  // c_lane is applied with the reference
+            xv[4 * i + r] = x;
+            continue;
+          }
           x = __fmul_rn(x, c_lane);
           xv[4 * i + r] = hvalid ? x : -INFINITY;
           if constexpr (DEBUG) {
@@ -933,18 +952,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
       }
     }
     const bool tail = t0 + kWTile > t_end;  // wave-uniform
+    if constexpr (V4) {
+      tail_tile = tail;  // finished outside the hot loop
+      return;
+    }
     if (tail) {
       const int k0 = t0 + 32 * part + 8 * grp;
 #pragma unroll
       for (int i = 0; i < 8; ++i) xv[i] = (k0 + i < t_end) ? xv[i] : -INFINITY;
       // weights past the range are 0; fp16 value bytes there could be inf or
       // NaN and are cleared, INT8 value bytes are always finite numbers
-      if constexpr (V4) mask_steps(k0, t_end, vr);
-      else if constexpr (!V8) mask_values(t0, t_end, lane, vr);
-    }
-    if constexpr (V4) {
-      const uint32_t top = max_pairs(max_pairs(vr.s.x, vr.s.y), max_pairs(vr.s.z, vr.s.w));
-      step_rises = max_pairs(top, step_top) != step_top;
+      if constexpr (VK == kValF16) mask_values(t0, t_end, lane, vr);
     }
 
     // ---- 3. integer running maximum per head ----
@@ -974,23 +992,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // element gets one exact power-of-two product. It runs outside the hot
   // loop below, so the accumulators stay in the matrix-core registers there.
   auto rescale = [&]() {
-    int e_down = 0;
-    if constexpr (V4) {
-      const uint32_t top = max_pairs(max_pairs(vr.s.x, vr.s.y), max_pairs(vr.s.z, vr.s.w));
-      const int bits = wave_max_i32((int)max(top & 0xFFFFu, top >> 16));
-      const float s = __half2float(__ushort_as_half((unsigned short)bits));
-      const int e = max(e_ref, s > 0.0f ? (int)__builtin_amdgcn_frexp_expf(s) : e_ref);
-      e_down = e_ref - e;
-      e_ref = e;
-      // 2^e as fp16: subnormal below 2^-14
-      step_top = (e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24)) * 0x00010001u;
-    }
     if (first) {  // nothing is summed yet
       m_run = m_new;
       return;
     }
-    const float f =
-        (m_run == INT_MIN) ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, m_run - m_new + e_down);
+    const float f = (m_run == INT_MIN) ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, m_run - m_new);
     const int arow = lane & 15, acol = lane >> 4;
 #pragma unroll
     for (int nb = 0; nb < kAcc; ++nb) {
@@ -1006,6 +1012,67 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     m_run = m_new;
   };
 
+  // 4-bit values: the tile's weights (in hw, lw) and their sums. True if one is out of
+  // range: the reference has to rise, nothing is summed yet.
+  float psum = 0.0f, pzsum = 0.0f;
+  auto weights4 = [&](bool tail, int k0) -> bool {
+    if constexpr (V4) {
+    const uint32_t sw[4] = {vr.s.x, vr.s.y, vr.s.z, vr.s.w};
+    const uint32_t zw[4] = {vr.z.x, vr.z.y, vr.z.z, vr.z.w};
+    float p[8], w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(xv[i], c_lane, bias4));
+    if (tail) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = k0 + i < t_end ? p[i] : 0.0f;
+    }
+    psum = 0.0f;
+    pzsum = 0.0f;
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float st = (float)__builtin_bit_cast(half2v, sw[i / 2])[i & 1];
+      const float z = (float)__builtin_bit_cast(half2v, zw[i / 2])[i & 1];
+      psum += p[i];
+      pzsum = __builtin_fmaf(p[i], __builtin_fmaf(st, 8.0f, z), pzsum);
+      w[i] = __builtin_fmaf(p[i], st, 0.0f);
+      most = fmaxf(most, w[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // operand order 0 2 1 3 4 6 5 7 (int4_value_fragment)
+      const float w0 = w[(i & 1) + 4 * (i >> 1)], w1 = w[(i & 1) + 4 * (i >> 1) + 2];
+      const half2v hi = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w0, w1));
+      hw[i] = __builtin_bit_cast(uint32_t, hi);
+      float l0 = __builtin_fmaf(neg_one, (float)hi.x, w0), l1 = __builtin_fmaf(neg_one, (float)hi.y, w1);
+      asm("" : "+v"(l0), "+v"(l1));  // one packed conversion, not two mixed multiply-adds
+      lw[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{l0, l1}), half2v));
+    }
+    return most > kMostWeight4;
+    }
+    return false;
+  };
+  // The reference that takes in the tile at hand: above x + log2 s of its keys.
+  auto raised4 = [&](bool tail, int k0) -> int {
+    if constexpr (V4) {
+    const uint32_t sw[4] = {vr.s.x, vr.s.y, vr.s.z, vr.s.w};
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float st = (float)__builtin_bit_cast(half2v, sw[i / 2])[i & 1];
+      const float x = __fmul_rn(xv[i], c_lane) + __builtin_amdgcn_logf(st);
+      if (!tail || k0 + i < t_end) mx = fmaxf(mx, x);
+    }
+    mx = fmaxf(mx, dpp_move<kDppRowRor8>(mx));
+    int mt = (hvalid && mx > -INFINITY) ? (int)ceilf(mx) : INT_MIN;
+    const auto r16 = __builtin_amdgcn_permlane16_swap((uint32_t)mt, (uint32_t)mt, false, false);
+    mt = max((int)r16[0], (int)r16[1]);
+    const auto r32 = __builtin_amdgcn_permlane32_swap((uint32_t)mt, (uint32_t)mt, false, false);
+    return max(m_run, max((int)r32[0], (int)r32[1]));
+    }
+    return m_run;
+  };
+
   // Stage 2 of a tile: weights from the scores and P.V on the matrix cores.
   auto stage2 = [&]() {
     // ---- 4. weights (fp16 high / low parts) and P.V on the matrix cores ----
@@ -1014,13 +1081,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     // rows 0-7 = hi, 8-15 = lo of the part-0 weights; block kb = 1 takes rows
     // 0-7 = lo, 8-15 = hi of the part-1 weights. Rows h and h + 8 are summed
     // at the end, so both blocks see hi + lo of every weight.
-    const float bias = hvalid ? (V4 ? kPScale - (float)e_ref : kPScale) - (float)m_run : 0.0f;
-    uint32_t hw[4], lw[4];
+    if constexpr (!V4) {
+    const float bias = hvalid ? kPScale - (float)m_run : 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float p0, p1;
-      // the two keys of an operand dword; 4-bit values have 0 2, 1 3, 4 6, 5 7
-      const int k0 = V4 ? (i & 1) + 4 * (i >> 1) : 2 * i, k1 = V4 ? k0 + 2 : k0 + 1;
       if constexpr (kPow2) {
         // A~ = 2^-k with k = M - ceil(x - 1/2) (M - x rounded half up):
         // p = 2^(ceil(x - 1/2) - M + 12), exact; keys masked to -inf get 0.
@@ -1037,20 +1102,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
         p0 = pw(xv[2 * i]);
         p1 = pw(xv[2 * i + 1]);
       } else {
-        p0 = __builtin_amdgcn_exp2f(xv[k0] + bias);
-        p1 = __builtin_amdgcn_exp2f(xv[k1] + bias);
-      }
-      if constexpr (V4) {
-        const uint32_t sw[4] = {vr.s.x, vr.s.y, vr.s.z, vr.s.w};
-        const uint32_t zw[4] = {vr.z.x, vr.z.y, vr.z.z, vr.z.w};
-        const half2v s0 = __builtin_bit_cast(half2v, sw[k0 / 2]), s1 = __builtin_bit_cast(half2v, sw[k1 / 2]);
-        const half2v z0 = __builtin_bit_cast(half2v, zw[k0 / 2]), z1 = __builtin_bit_cast(half2v, zw[k1 / 2]);
-        lsum += p0;
-        lsum += p1;
-        zsum = __builtin_fmaf(p0, __builtin_fmaf((float)s0[k0 & 1], 8.0f, (float)z0[k0 & 1]), zsum);
-        zsum = __builtin_fmaf(p1, __builtin_fmaf((float)s1[k1 & 1], 8.0f, (float)z1[k1 & 1]), zsum);
-        p0 = __fmul_rn(p0, (float)s0[k0 & 1]);
-        p1 = __fmul_rn(p1, (float)s1[k1 & 1]);
+        p0 = __builtin_amdgcn_exp2f(xv[2 * i] + bias);
+        p1 = __builtin_amdgcn_exp2f(xv[2 * i + 1] + bias);
       }
       if constexpr (V8) {
         // the softmax sum takes p; A.V takes p 2^(g_ref - g) (exact scaling)
@@ -1066,9 +1119,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
                          (_Float16)__builtin_fmaf(neg_one, (float)hi.y, p1)};
       lw[i] = __builtin_bit_cast(uint32_t, lo);
     }
+    } else {
+      lsum += psum;
+      zsum += pzsum;
+    }
     uint32_t a0w[4], a1w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      if constexpr (V4) {  // the move and the choice in one: lanes of the other part keep hw
+        a0w[i] = (uint32_t)__builtin_amdgcn_update_dpp((int)hw[i], (int)lw[i], kDppRowRor8, 0xF, 0xC, false);
+        a1w[i] = (uint32_t)__builtin_amdgcn_update_dpp((int)hw[i], (int)lw[i], kDppRowRor8, 0xF, 0x3, false);
+        continue;
+      }
       const uint32_t rl =
           (uint32_t)__builtin_amdgcn_mov_dpp((int)lw[i], kDppRowRor8, 0xF, 0xF, true);
       a0w[i] = part ? rl : hw[i];
@@ -1131,13 +1193,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
 #pragma nounroll
     for (;;) {
       stage1(kr[0], kr[1], j);
-      if (__any(m_new != m_run || step_rises)) break;
+      if constexpr (V4) {
+        if (tail_tile) break;
+        least_steps(vr);
+        if (__any(weights4(false, 0))) break;
+      } else {
+        if (__any(m_new != m_run)) break;
+      }
       stage2();
       advance();
       if (j >= n_tiles) break;
     }
     if (j >= n_tiles) break;
-    rescale();
+    if constexpr (V4) {
+      const int k0 = t_begin + kWTile * j + 32 * part + 8 * grp;
+      if (tail_tile) mask_steps(k0, t_end, vr);
+      least_steps(vr);
+      m_new = raised4(tail_tile, k0);
+      rescale();
+      bias4 = hvalid ? kPScale4 - (float)m_run : 0.0f;
+      weights4(tail_tile, k0);
+    } else {
+      rescale();
+    }
     stage2();
     advance();
   }
@@ -1158,11 +1236,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
         const float sum = __uint_as_float(h[0]) + __uint_as_float(h[1]);
         if (lane < 32) sm.wo[wave][4 * grp + r][16 * nb + row] = sum;
       }
-  }
-  // 4-bit values: the sums' reference is 2^(m_run + e_ref) (in range: a score beyond
-  // 2^31 has saturated)
-  if constexpr (V4) {
-    if (m_run != INT_MIN) m_run = min(max(m_run, INT_MIN + 64), INT_MAX - 64) + e_ref;
   }
   if (lane < 8) sm.wm[wave][lane] = m_run;
   if constexpr (V4) {

@@ -174,6 +174,79 @@ __device__ __forceinline__ f32x4 score_set(const uint32_t (&w)[4], const uint32_
   return d;
 }
 
+// The same sums with the shifts in the operand: fp4 holds the powers of two 1/2, 1, 2 and
+// 4, so one operand takes the elements of four exponents, and two operands (e = 3 .. 6 at
+// positions 0 .. 3 and e = 0 .. 2 at 4 .. 6) all of a term: 0 or a signed power of two per
+// element, whose product with q^ is the shifted q^. A PoT-Mk magnitude is its leading
+// power of two and one more, b - k positions lower, for every mantissa bit b that is set:
+// 2 (k + 1) operands instead of the 7 + k of one bit position each, and still no value that
+// is not a power of two. 8 matrix instructions of a tile's scores instead of 28 at k = 0, 16
+// instead of 32 at k = 1, 24 instead of 36 at k = 2 (from k = 3 on 32 instead of 40: no
+// gain). With 4-bit values the matrix cores' power decides how long a full chip takes: B
+// = 64, T = 32768, PoT-4 161 us with a ternary operand per position.
+//
+// The operand nibbles are looked up, four at a time, by v_perm_b32.
+__device__ __forceinline__ uint32_t lookup_nibbles(uint32_t even, uint32_t odd, uint32_t lut0,
+                                                   uint32_t lut1) {
+  return __builtin_amdgcn_perm(lut1, lut0, even) | __builtin_amdgcn_perm(lut1, lut0, odd) << 4;
+}
+// Mantissa bit B: the powers of the elements whose bit is set (pl[B], bit 4 i + c of it for
+// nibble i of dword c), from position B on.
+template <int B>
+__device__ __forceinline__ void add_term(const uint32_t* pl, const uint32_t (&low)[4],
+                                         const uint32_t (&high)[4], const uint32_t (&sign)[4],
+                                         const PlaneQuery& q, f32x4& d) {
+  uint32_t mask[4], t[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t bit = (pl[B] >> c) & 0x11111111u;
+    mask[c] = (bit << 3) - bit;  // the nibble's three magnitude bits
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    t[c] = __builtin_amdgcn_bitop3_b32(low[c], mask[c], sign[c], kMaskOrTable);
+  add_plane<B + 1>(t, q, d);
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    t[c] = __builtin_amdgcn_bitop3_b32(high[c], mask[c], sign[c], kMaskOrTable);
+  add_plane<B + 5>(t, q, d);
+}
+template <int K>
+__device__ __forceinline__ f32x4 score_set_powers(const uint32_t (&w)[4], const uint32_t* pl,
+                                                  const PlaneQuery& q) {
+  // fp4 codes of e = 0 .. 3 and 4 .. 7, a byte each
+  constexpr uint32_t kLow0 = 0x06000000u, kLow1 = 0x00010204u;   // e = 3: 4, .. e = 6: 1/2
+  constexpr uint32_t kHigh0 = 0x00010204u, kHigh1 = 0u;          // e = 0: 2, .. e = 2: 1/2
+  uint32_t c4[4];
+  if constexpr (K == 0) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) c4[c] = w[c];
+  } else {
+    transpose_codes(w, c4);
+  }
+  uint32_t low[4], high[4], sign[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t even = c4[c] & 0x07070707u, odd = (c4[c] >> 4) & 0x07070707u;
+    low[c] = lookup_nibbles(even, odd, kLow0, kLow1);
+    high[c] = lookup_nibbles(even, odd, kHigh0, kHigh1);
+    sign[c] = c4[c] & 0x88888888u;
+  }
+  f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+  uint32_t t[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) t[c] = low[c] | sign[c];
+  add_plane<K + 1>(t, q, d);  // 1/2 of position K + 1 is position K: e = 6
+#pragma unroll
+  for (int c = 0; c < 4; ++c) t[c] = high[c] | sign[c];
+  add_plane<K + 5>(t, q, d);
+  if constexpr (K >= 1) add_term<0>(pl, low, high, sign, q, d);
+  if constexpr (K >= 2) add_term<1>(pl, low, high, sign, q, d);
+  if constexpr (K >= 3) add_term<2>(pl, low, high, sign, q, d);
+  if constexpr (K >= 4) add_term<3>(pl, low, high, sign, q, d);
+  return d;
+}
+
 // One element of q^ of one head as hi and lo (q^ = 16 hi + lo, hi in [-8, 8],
 // lo in [-8, 7]) at its place in the operand order; the head's 64 elements
 // make two blocks of 32.
