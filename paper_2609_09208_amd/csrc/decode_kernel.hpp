@@ -406,6 +406,19 @@ __device__ __forceinline__ void mask_values(int t0, int t_end, int lane, ValRegs
   }
 }
 
+// z + 8 s in fp32 from the fp16 halves `hi` of their dwords, by one mixed multiply-add (the
+// compiler converts s first).
+__device__ __forceinline__ float step8_plus(uint32_t s, uint32_t z, bool hi) {
+  float c;
+  if (hi)
+    asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel:[1,0,1] op_sel_hi:[1,0,1]"
+        : "=v"(c) : "v"(s), "s"(8.0f), "v"(z));
+  else
+    asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel:[0,0,0] op_sel_hi:[1,0,1]"
+        : "=v"(c) : "v"(s), "s"(8.0f), "v"(z));
+  return c;
+}
+
 // Steps of 0 (constant rows, and keys past the range) as 2^-24, fp16's smallest number.
 __device__ __forceinline__ void least_steps(ValRegs<kValI4>& v) {
   const uint32_t least = 0x00010001u;
@@ -762,6 +775,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   if constexpr (MODE == kScorePot) asm("" : "+v"(m22));
 
   KeyRegs<MODE, K> kr[2];
+  constexpr int kNext = V4 ? 0 : 1;  // where the next tile's keys go
   const int g_last = (t_end - 1) & ~7;  // first token of the range's last 8-token group
   Streams st{};
   st.t_end = t_end;
@@ -893,7 +907,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     const int t0 = t_begin + kWTile * jt;
     // the next tile's keys (past the range: the last tile again, unused)
     const int jl = min(kPool ? jn : jt + NW, j_last);
-    load_keys_tile(jl, knext);
+    if constexpr (!V4) load_keys_tile(jl, knext);
     if constexpr (kPool) {
       // claim the tile after jn now; it is needed one tile from now
       jc = jn + NW;
@@ -927,6 +941,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
       // keeps the matrix instructions above here (and so their operands' live
       // ranges short): the compiler would sink them to their first use
       asm volatile("" : "+v"(d[0]), "+v"(d[1]));
+      // 4-bit values: the codes have become operands, and their registers take the next
+      // tile's (requested before the scores they took eight more and as many moves)
+      if constexpr (V4) load_keys_tile(jl, knext);
       if constexpr (kEarlyV < 2) load_values_buf<VK, kEarlyV, 2>(st, t0, lane, vr);
       // ---- 2. scores to the log2 domain ----
 #pragma unroll
@@ -1026,15 +1043,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = k0 + i < t_end ? p[i] : 0.0f;
     }
-    psum = 0.0f;
-    pzsum = 0.0f;
     float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float st = (float)__builtin_bit_cast(half2v, sw[i / 2])[i & 1];
-      const float z = (float)__builtin_bit_cast(half2v, zw[i / 2])[i & 1];
-      psum += p[i];
-      pzsum = __builtin_fmaf(p[i], __builtin_fmaf(st, 8.0f, z), pzsum);
+      psum = i == 0 ? p[0] : psum + p[i];
+      const float c = step8_plus(sw[i / 2], zw[i / 2], i & 1);
+      pzsum = i == 0 ? p[0] * c : __builtin_fmaf(p[i], c, pzsum);
       w[i] = __builtin_fmaf(p[i], st, 0.0f);
       most = fmaxf(most, w[i]);
     }
@@ -1122,6 +1137,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     } else {
       lsum += psum;
       zsum += pzsum;
+      // now, so that the steps' and minima's registers are free for the next tile's
+      asm volatile("" : "+v"(lsum), "+v"(zsum));
     }
     uint32_t a0w[4], a1w[4];
 #pragma unroll
@@ -1173,7 +1190,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // times per wave). The prefetched registers move forward after each tile so
   // that every tile uses the same registers.
   auto advance = [&]() {
-    kr[0] = kr[1];
+    if constexpr (!V4) kr[0] = kr[1];
     // also after a tile that raised nothing: scores at -2^31, whose ceiling is INT_MIN
     // itself, have had their weights summed, and a later maximum takes them out
     first = false;
@@ -1192,7 +1209,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   while (j < n_tiles) {
 #pragma nounroll
     for (;;) {
-      stage1(kr[0], kr[1], j);
+      stage1(kr[0], kr[kNext], j);
       if constexpr (V4) {
         if (tail_tile) break;
         least_steps(vr);

@@ -185,30 +185,31 @@ __device__ __forceinline__ f32x4 score_set(const uint32_t (&w)[4], const uint32_
 // gain). With 4-bit values the matrix cores' power decides how long a full chip takes: B
 // = 64, T = 32768, PoT-4 161 us with a ternary operand per position.
 //
-// The operand nibbles are looked up, four at a time, by v_perm_b32.
-__device__ __forceinline__ uint32_t lookup_nibbles(uint32_t even, uint32_t odd, uint32_t lut0,
-                                                   uint32_t lut1) {
-  return __builtin_amdgcn_perm(lut1, lut0, even) | __builtin_amdgcn_perm(lut1, lut0, odd) << 4;
+// The operand nibbles are looked up, four at a time, by v_perm_b32: those of even elements
+// in bytes' low halves, of odd ones from the same table four bits up.
+constexpr uint32_t kOr3Table = 0xFE;  // a | b | c
+template <uint32_t LUT0, uint32_t LUT1>
+__device__ __forceinline__ uint32_t lookup_nibbles(uint32_t even, uint32_t odd, uint32_t sign) {
+  return __builtin_amdgcn_bitop3_b32(__builtin_amdgcn_perm(LUT1, LUT0, even),
+                                     __builtin_amdgcn_perm(LUT1 << 4, LUT0 << 4, odd), sign,
+                                     kOr3Table);
 }
 // Mantissa bit B: the powers of the elements whose bit is set (pl[B], bit 4 i + c of it for
 // nibble i of dword c), from position B on.
 template <int B>
 __device__ __forceinline__ void add_term(const uint32_t* pl, const uint32_t (&low)[4],
-                                         const uint32_t (&high)[4], const uint32_t (&sign)[4],
-                                         const PlaneQuery& q, f32x4& d) {
+                                         const uint32_t (&high)[4], const PlaneQuery& q, f32x4& d) {
   uint32_t mask[4], t[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const uint32_t bit = (pl[B] >> c) & 0x11111111u;
-    mask[c] = (bit << 3) - bit;  // the nibble's three magnitude bits
+    mask[c] = (bit << 4) - bit;  // the nibble (mod 2^32: bit 28's too)
   }
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
-    t[c] = __builtin_amdgcn_bitop3_b32(low[c], mask[c], sign[c], kMaskOrTable);
+  for (int c = 0; c < 4; ++c) t[c] = low[c] & mask[c];
   add_plane<B + 1>(t, q, d);
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
-    t[c] = __builtin_amdgcn_bitop3_b32(high[c], mask[c], sign[c], kMaskOrTable);
+  for (int c = 0; c < 4; ++c) t[c] = high[c] & mask[c];
   add_plane<B + 5>(t, q, d);
 }
 template <int K>
@@ -228,22 +229,17 @@ __device__ __forceinline__ f32x4 score_set_powers(const uint32_t (&w)[4], const 
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const uint32_t even = c4[c] & 0x07070707u, odd = (c4[c] >> 4) & 0x07070707u;
-    low[c] = lookup_nibbles(even, odd, kLow0, kLow1);
-    high[c] = lookup_nibbles(even, odd, kHigh0, kHigh1);
     sign[c] = c4[c] & 0x88888888u;
+    low[c] = lookup_nibbles<kLow0, kLow1>(even, odd, sign[c]);
+    high[c] = lookup_nibbles<kHigh0, kHigh1>(even, odd, sign[c]);
   }
   f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
-  uint32_t t[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) t[c] = low[c] | sign[c];
-  add_plane<K + 1>(t, q, d);  // 1/2 of position K + 1 is position K: e = 6
-#pragma unroll
-  for (int c = 0; c < 4; ++c) t[c] = high[c] | sign[c];
-  add_plane<K + 5>(t, q, d);
-  if constexpr (K >= 1) add_term<0>(pl, low, high, sign, q, d);
-  if constexpr (K >= 2) add_term<1>(pl, low, high, sign, q, d);
-  if constexpr (K >= 3) add_term<2>(pl, low, high, sign, q, d);
-  if constexpr (K >= 4) add_term<3>(pl, low, high, sign, q, d);
+  add_plane<K + 1>(low, q, d);  // 1/2 of position K + 1 is position K: e = 6
+  add_plane<K + 5>(high, q, d);
+  if constexpr (K >= 1) add_term<0>(pl, low, high, q, d);
+  if constexpr (K >= 2) add_term<1>(pl, low, high, q, d);
+  if constexpr (K >= 3) add_term<2>(pl, low, high, q, d);
+  if constexpr (K >= 4) add_term<3>(pl, low, high, q, d);
   return d;
 }
 
