@@ -265,13 +265,19 @@ typedef struct pot_rope {
   uint8_t axis_of_pair[32];
 } pot_rope;
 
-/* The rows of one part of a projection: element m of head h of token t of batch row
- * b is data[b * stride_b + t * stride_s + h * stride_h + m] (strides in elements; 0 or
- * negative ones may be given). */
-typedef struct pot_rows {
-  const void* data;
+/* One part of a projection: its queries, keys or values.
+ *  rows    element m of head h of token t of batch row b is rows[b * stride_b +
+ *          t * stride_s + h * stride_h + m] (strides in elements; 0 or negative ones may
+ *          be given). Device, 16-byte aligned like every row (the strides of dimensions
+ *          over 1). NULL: the part is left out.
+ *  weight  [64], device, 16-byte aligned, or NULL: no norm.
+ *  out     dense [B][heads][S][64], device, 16-byte aligned; NULL iff rows is. */
+typedef struct pot_part {
+  const void* rows;
   int64_t stride_b, stride_s, stride_h;
-} pot_rows;
+  const void* weight;
+  void* out;
+} pot_part;
 
 /* Norm of queries and keys per head and their position rotation, in one pass from
  * the rows of a QKV projection to what the cache writers and the decode calls take:
@@ -280,30 +286,23 @@ typedef struct pot_rows {
  * for pair i with the position on its axis. Values v pass as they are. All in fp32
  * (the angle in fp64, so that far positions keep their place in the turn), one
  * rounding at the end.
- *  dtype        pot_dtype of q, k and v.
- *  q, k, v      host structs of device rows: [B][S][Hq], [B][S][Hkv] and [B][S][Hkv]
- *               rows of 64 elements, e.g. the parts of one packed projection. A NULL
- *               struct or data leaves the part out; its output must then be NULL too.
- *               Rows must be 16-byte aligned (data, and the strides of dimensions
- *               over 1).
- *  q_weight, k_weight [64] of weight_dtype, device, 16-byte aligned, or NULL: no norm of
- *               that part.
+ *  dtype        pot_dtype of the rows.
+ *  parts        HOST array {q, k, v}: [B][S][Hq], [B][S][Hkv] and [B][S][Hkv] rows of 64
+ *               elements, e.g. the parts of one packed projection. q's output is of
+ *               q_out_dtype (pot_decode_attention takes fp32 with S = 1); k's and v's are
+ *               fp16 (dense rows for pot_encode_keys and the value stores; S = 1: k_new
+ *               and v_new of the append calls). v takes no weight.
+ *  weight_dtype pot_dtype of the weights.
  *  eps          finite, >= 0.
  *  positions    int64 [n_axes][B][S], device, any sign (8-byte aligned; NULL iff
  *               rot_dim = 0). The angle is exact to 2^-52 of itself plus rounding: for
  *               |position * inv_freq| up to 2^31 within 1e-6.
  *  inv_freq     double [rot_dim/2], device: radians per position (NULL iff rot_dim = 0).
- *  q_out        [B][Hq][S][64] of q_out_dtype (pot_decode_attention takes fp32 with
- *               S = 1).
- *  k_out, v_out fp16 [B][Hkv][S][64] (dense rows for pot_encode_keys and the value
- *               stores; S = 1: k_new and v_new of the append calls).
- * Outputs are 16-byte aligned and alias nothing. B or S of 0 is a no-op. */
-pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
-                         const pot_rows* k, const pot_rows* v, const void* q_weight,
-                         const void* k_weight, int32_t weight_dtype, float eps,
-                         const int64_t* positions, const double* inv_freq, int32_t B, int32_t S,
-                         int32_t Hq, int32_t Hkv, int32_t q_out_dtype, void* q_out,
-                         uint16_t* k_out, uint16_t* v_out, void* stream);
+ * Outputs alias nothing. B or S of 0 is a no-op; B * S up to 2^31. */
+pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* parts,
+                         int32_t weight_dtype, float eps, const int64_t* positions,
+                         const double* inv_freq, int32_t B, int32_t S, int32_t Hq, int32_t Hkv,
+                         int32_t q_out_dtype, void* stream);
 
 /* Workspace bytes pot_decode_attention needs for this problem shape: the
  * key-split partials (M_s, l_s, o_s) for the largest split count the planner

@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch  # its HIP runtime has to be loaded before the library (see _load_library)
@@ -55,9 +56,10 @@ class pot_rope(ctypes.Structure):
                 ("axis_of_pair", ctypes.c_uint8 * 32)]
 
 
-class pot_rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
-                ("stride_s", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+class pot_part(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_s", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p)]
 
 
 POT_FP16, POT_BF16, POT_FP32 = 0, 1, 2
@@ -126,8 +128,8 @@ def _load_library():
         "pot_load_values": (i32, [P, i64, i64, i64, i64, P, P]),
         "pot_load_values_int8": (i32, [P, P, i64, i64, i64, i64, P, P]),
         "pot_load_values_int4": (i32, [P, i64, i64, i64, i64, P, P]),
-        "pot_norm_rope": (i32, [ctypes.POINTER(pot_rope), i32, P, P, P, P, P, i32,
-                                ctypes.c_float, P, P, i32, i32, i32, i32, i32, P, P, P, P]),
+        "pot_norm_rope": (i32, [ctypes.POINTER(pot_rope), i32, P, i32, ctypes.c_float, P, P, i32,
+                                i32, i32, i32, i32, P]),
         "pot_int8_encode_keys": (i32, [P, i64, i64, i32, P, P, P]),
         "pot_int8_decode_attention": (i32, [P, P, P, P, i64, P, i32, i32, i32,
                                             i32, i32, P, P, S, dbg_p, P]),
@@ -368,28 +370,32 @@ def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new
 
 
 _DTYPES = {torch.float16: POT_FP16, torch.bfloat16: POT_BF16, torch.float32: POT_FP32}
-_Rows3 = ctypes.c_int64 * 12  # three pot_rows
-_ROWS_BYTES = ctypes.sizeof(pot_rows)
+_pack_parts = struct.Struct("18q").pack  # three pot_part
+_NO_PART = (0, 0, 0, 0, 0, 0)
 
 
 def _mismatch(what: str):
     raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", what)
 
 
-def _part(x, out, B: int, S: int, out_type):
-    """Heads, address and strides of a part of a projection [B, S, heads, 64] (any strides,
-    elements side by side) whose output is dense [B, heads, S, 64] (of out_type, if given)."""
+def _part(x, weight, out, B: int, S: int, dtype, out_type):
+    """The fields of pot_part of a projection's rows [B, S, heads, 64] (any strides, elements
+    side by side) whose output is dense [B, heads, S, 64] (of out_type, if given), and its
+    heads."""
     b, s, h, d = x.shape
     sb, ss, sh, se = x.stride()
-    if b != B or s != S or d != HEAD_DIM or se != 1:
-        _mismatch("rows [B, S, heads, 64] with dense elements are needed")
+    if b != B or s != S or d != HEAD_DIM or se != 1 or x.dtype is not dtype:
+        _mismatch("rows [B, S, heads, 64] of one type with dense elements are needed")
     if (out is None or out.numel() != B * h * S * HEAD_DIM or not out.is_contiguous()
             or (out_type is not None and out.dtype is not out_type)):
         _mismatch("a dense output [B, heads, S, 64] is needed (k and v: float16)")
-    return h, x.data_ptr(), sb, ss, sh
-
-
-_NO_PART = (0, 0, 0, 0, 0)
+    if weight is None:
+        w = 0
+    else:
+        if weight.numel() != HEAD_DIM or not weight.is_contiguous():
+            _mismatch("weights are [64] and dense")
+        w = weight.data_ptr()
+    return h, x.data_ptr(), sb, ss, sh, w, out.data_ptr()
 
 
 def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions, inv_freq,
@@ -401,39 +407,30 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
     first = q if q is not None else k if k is not None else v
     if first is None:
         return
-    B, S = first.shape[:2]
-    dtype = first.dtype
-    hq, *at_q = _NO_PART if q is None else _part(q, q_out, B, S, None)
-    hk, *at_k = _NO_PART if k is None else _part(k, k_out, B, S, torch.float16)
-    hv, *at_v = _NO_PART if v is None else _part(v, v_out, B, S, torch.float16)
+    B, S, _, _ = first.shape
+    dtype, types = first.dtype, _DTYPES
+    hq, *at_q = (0, *_NO_PART) if q is None else _part(q, q_weight, q_out, B, S, dtype, None)
+    hk, *at_k = (0, *_NO_PART) if k is None else _part(k, k_weight, k_out, B, S, dtype,
+                                                       torch.float16)
+    hv, *at_v = (0, *_NO_PART) if v is None else _part(v, None, v_out, B, S, dtype, torch.float16)
     if hk and hv and hk != hv:
         _mismatch("k and v have the same number of heads")
-    if (k is not None and k.dtype is not dtype) or (v is not None and v.dtype is not dtype):
-        _mismatch("q, k and v are of one type")
-    wtype = None
-    for w in (q_weight, k_weight):
-        if w is not None:
-            if (w.numel() != HEAD_DIM or not w.is_contiguous()
-                    or (wtype is not None and w.dtype is not wtype)):
-                _mismatch("weights are [64], dense and of one type")
-            wtype = w.dtype
+    w = q_weight if q_weight is not None else k_weight
+    if k_weight is not None and k_weight.dtype is not w.dtype:
+        _mismatch("weights are of one type")
     if positions is not None and (positions.dtype is not torch.int64 or not positions.is_contiguous()
                                   or positions.numel() != rope.n_axes * B * S):
         _mismatch("positions are dense int64 [n_axes, B, S]")
     if inv_freq is not None and (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
                                  or inv_freq.numel() < rope.rot_dim // 2):
         _mismatch("inv_freq is dense float64 [rot_dim / 2]")
-    types = _DTYPES
     qtype = types.get(q_out.dtype) if q_out is not None else POT_FP32
-    itype, wtype = types.get(dtype), types.get(wtype) if wtype is not None else POT_FP32
+    itype, wtype = types.get(dtype), types.get(w.dtype) if w is not None else POT_FP32
     if qtype is None or itype is None or wtype is None:
         _mismatch("types are float16, bfloat16 or float32")
-    rows = _Rows3(*at_q, *at_k, *at_v)
-    at = ctypes.addressof(rows)
-    _check(_lib.pot_norm_rope(
-        ctypes.byref(rope), itype, at, at + _ROWS_BYTES, at + 2 * _ROWS_BYTES, _ptr(q_weight),
-        _ptr(k_weight), wtype, eps, _ptr(positions), _ptr(inv_freq), B, S, hq, hk or hv, qtype,
-        _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream)))
+    _check(_lib.pot_norm_rope(ctypes.byref(rope), itype, _pack_parts(*at_q, *at_k, *at_v), wtype,
+                              eps, _ptr(positions), _ptr(inv_freq), B, S, hq, hk or hv, qtype,
+                              _stream(stream)))
 
 
 def pot_ds4a_decode_attention(fmt: pot_format, q, codes_se, key_scale, v_fp16, t_cap: int,

@@ -477,21 +477,21 @@ pot_status load_values(int format, const void* cache, const int8_t* v_exp, int64
 }
 
 // One part of a projection and its output: both given, or neither.
-pot_status check_part(const char* name, const pot_rows* r, const void* out, int32_t heads,
-                      int32_t B, int32_t S, int size, RowsIn* in) {
+pot_status check_part(const char* name, const pot_part& p, int32_t heads, int32_t B, int32_t S,
+                      int size, RowsIn* in) {
   *in = RowsIn{};
-  if (!r || !r->data) {
-    if (out) return fail(POT_ERR_INVALID_ARG, "%s is left out, but not its output", name);
+  if (!p.rows) {
+    if (p.out) return fail(POT_ERR_INVALID_ARG, "%s is left out, but not its output", name);
     return POT_OK;
   }
-  if (!out) return fail(POT_ERR_INVALID_ARG, "%s has no output", name);
+  if (!p.out) return fail(POT_ERR_INVALID_ARG, "%s has no output", name);
   if (heads < 1) return fail(POT_ERR_INVALID_ARG, "%d heads of %s", heads, name);
   const int64_t per16 = 16 / size;
-  if (!aligned(r->data, 16) || !aligned(out, 16) || (B > 1 && r->stride_b % per16) ||
-      (S > 1 && r->stride_s % per16) || (heads > 1 && r->stride_h % per16))
-    return fail(POT_ERR_INVALID_ARG, "rows of %s and its output must be 16-byte aligned", name);
-  *in = RowsIn{r->data, B > 1 ? r->stride_b : 0, S > 1 ? r->stride_s : 0,
-               heads > 1 ? r->stride_h : 0};
+  if (!aligned(p.rows, 16) || !aligned(p.out, 16) || !aligned(p.weight, 16) ||
+      (B > 1 && p.stride_b % per16) || (S > 1 && p.stride_s % per16) ||
+      (heads > 1 && p.stride_h % per16))
+    return fail(POT_ERR_INVALID_ARG, "rows, weight and output of %s must be 16-byte aligned", name);
+  *in = RowsIn{p.rows, B > 1 ? p.stride_b : 0, S > 1 ? p.stride_s : 0, heads > 1 ? p.stride_h : 0};
   return POT_OK;
 }
 
@@ -637,13 +637,11 @@ pot_status pot_load_values_int4(const uint8_t* v_u4, int64_t n_seq, int64_t n_to
   return load_values(2, v_u4, nullptr, n_seq, n_tok, t_cap, t0, v_fp16, stream);
 }
 
-pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
-                         const pot_rows* k, const pot_rows* v, const void* q_weight,
-                         const void* k_weight, int32_t weight_dtype, float eps,
-                         const int64_t* positions, const double* inv_freq, int32_t B, int32_t S,
-                         int32_t Hq, int32_t Hkv, int32_t q_out_dtype, void* q_out,
-                         uint16_t* k_out, uint16_t* v_out, void* stream) {
-  if (!rope) return fail(POT_ERR_INVALID_ARG, "rope is NULL");
+pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* parts,
+                         int32_t weight_dtype, float eps, const int64_t* positions,
+                         const double* inv_freq, int32_t B, int32_t S, int32_t Hq, int32_t Hkv,
+                         int32_t q_out_dtype, void* stream) {
+  if (!rope || !parts) return fail(POT_ERR_INVALID_ARG, "rope or parts is NULL");
   if (rope->head_dim != 64)
     return fail(POT_ERR_UNSUPPORTED, "head_dim %d (only 64)", rope->head_dim);
   const int r = rope->rot_dim;
@@ -666,26 +664,25 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_rows* q,
   if (B == 0 || S == 0) return ok();
   NormRopeArgs a{};
   const int size = dtype == POT_FP32 ? 4 : 2;
-  pot_status st = check_part("q", q, q_out, Hq, B, S, size, &a.q);
-  if (st == POT_OK) st = check_part("k", k, k_out, Hkv, B, S, size, &a.k);
-  if (st == POT_OK) st = check_part("v", v, v_out, Hkv, B, S, size, &a.v);
+  pot_status st = check_part("q", parts[0], Hq, B, S, size, &a.q);
+  if (st == POT_OK) st = check_part("k", parts[1], Hkv, B, S, size, &a.k);
+  if (st == POT_OK) st = check_part("v", parts[2], Hkv, B, S, size, &a.v);
   if (st != POT_OK) return st;
+  if (parts[2].weight) return fail(POT_ERR_INVALID_ARG, "v takes no weight");
   if (!a.q.data && !a.k.data && !a.v.data) return ok();
   if (r > 0 && (a.q.data || a.k.data) && (!positions || !inv_freq))
     return fail(POT_ERR_INVALID_ARG, "positions or inv_freq is NULL");
   if (!aligned(positions, 8) || !aligned(inv_freq, 8))
     return fail(POT_ERR_INVALID_ARG, "positions and inv_freq must be 8-byte aligned");
-  if (!aligned(q_weight, 16) || !aligned(k_weight, 16))
-    return fail(POT_ERR_INVALID_ARG, "q_weight and k_weight must be 16-byte aligned");
   if ((int64_t)B * S > ((int64_t)1 << 31))
     return fail(POT_ERR_INVALID_ARG, "B * S too large");
-  a.q_weight = a.q.data ? q_weight : nullptr;
-  a.k_weight = a.k.data ? k_weight : nullptr;
+  a.q_weight = a.q.data ? parts[0].weight : nullptr;
+  a.k_weight = a.k.data ? parts[1].weight : nullptr;
   a.positions = positions;
   a.inv_freq = inv_freq;
-  a.q_out = q_out;
-  a.k_out = k_out;
-  a.v_out = v_out;
+  a.q_out = parts[0].out;
+  a.k_out = static_cast<uint16_t*>(parts[1].out);
+  a.v_out = static_cast<uint16_t*>(parts[2].out);
   a.eps = eps;
   a.B = B;
   a.S = S;

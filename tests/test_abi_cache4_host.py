@@ -104,15 +104,15 @@ def test_key_read_back_refuses_formats():
 
 def _rope(**over):
     rope = dict(rot_dim=64, neighbours=0, n_axes=1, head_dim=64, axis=[0] * 32)
-    a = dict(dtype=1, q=FAKE, k=FAKE, v=FAKE, sq=(64, 64, 64), qw=FAKE, kw=FAKE, wt=2, eps=1e-6, pos=FAKE, inv=FAKE, B=2,
-             S=3, Hq=4, Hkv=2, qt=2, qo=FAKE, ko=FAKE, vo=FAKE)
+    a = dict(dtype=1, q=FAKE, k=FAKE, v=FAKE, sq=(64, 64, 64), qw=FAKE, kw=FAKE, vw=None, wt=2, eps=1e-6, pos=FAKE, inv=FAKE,
+             B=2, S=3, Hq=4, Hkv=2, qt=2, qo=FAKE, ko=FAKE, vo=FAKE)
     for n, x in over.items():
         (rope if n in rope else a)[n] = x
     r = pa.pot_rope(rope["head_dim"], rope["rot_dim"], rope["neighbours"], rope["n_axes"], (ctypes.c_uint8 * 32)(*rope["axis"]))
-    part = lambda p, s=(64, 64, 64): ctypes.byref(pa.pot_rows(p, *s)) if p != "none" else None  # noqa: E731
-    return pa._lib.pot_norm_rope(ctypes.byref(r), a["dtype"], part(a["q"], a["sq"]), part(a["k"]), part(a["v"]), a["qw"],
-                                 a["kw"], a["wt"], a["eps"], a["pos"], a["inv"], a["B"], a["S"], a["Hq"], a["Hkv"], a["qt"],
-                                 a["qo"], a["ko"], a["vo"], None)
+    parts = (pa.pot_part * 3)(pa.pot_part(a["q"], *a["sq"], a["qw"], a["qo"]), pa.pot_part(a["k"], 64, 64, 64, a["kw"], a["ko"]),
+                              pa.pot_part(a["v"], 64, 64, 64, a["vw"], a["vo"]))
+    return pa._lib.pot_norm_rope(ctypes.byref(r), a["dtype"], ctypes.byref(parts), a["wt"], a["eps"], a["pos"], a["inv"], a["B"],
+                                 a["S"], a["Hq"], a["Hkv"], a["qt"], None)
 
 
 @pytest.mark.parametrize("over,code", [
@@ -121,7 +121,7 @@ def _rope(**over):
     (dict(dtype=3), INVALID), (dict(wt=-1), INVALID), (dict(qt=9), INVALID), (dict(eps=-1.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(B=-1), INVALID), (dict(Hq=0), INVALID),
     (dict(Hkv=0), INVALID), (dict(qo=None), INVALID), (dict(ko=None), INVALID), (dict(vo=None), INVALID), (dict(q=None), INVALID),
-    (dict(k="none"), INVALID), (dict(q=FAKE + 2), INVALID), (dict(ko=FAKE + 8), INVALID), (dict(sq=(4, 64, 64)), INVALID),
+    (dict(k=None), INVALID), (dict(vw=FAKE), INVALID), (dict(kw=FAKE + 8), INVALID), (dict(q=FAKE + 2), INVALID), (dict(ko=FAKE + 8), INVALID), (dict(sq=(4, 64, 64)), INVALID),
     (dict(sq=(64, 4, 64)), INVALID), (dict(sq=(64, 64, 4)), INVALID), (dict(pos=None), INVALID), (dict(inv=None), INVALID),
     (dict(pos=FAKE + 4), INVALID), (dict(inv=FAKE + 4), INVALID), (dict(qw=FAKE + 2), INVALID),
     (dict(B=1 << 16, S=1 << 16), INVALID),
@@ -133,9 +133,9 @@ def test_norm_rope_refuses(over, code):
 
 def test_norm_rope_of_nothing():
     assert _rope(B=0) == pa.POT_OK and _rope(S=0) == pa.POT_OK
-    assert _rope(q=None, k="none", v=None, qo=None, ko=None, vo=None) == pa.POT_OK
-    assert pa._lib.pot_norm_rope(None, 1, None, None, None, None, None, 2, 0.0, None, None, 1, 1, 1, 1, 2, None, None, None,
-                                 None) == INVALID
+    assert _rope(q=None, k=None, v=None, qo=None, ko=None, vo=None) == pa.POT_OK
+    assert pa._lib.pot_norm_rope(None, 1, None, 2, 0.0, None, None, 1, 1, 1, 1, 2, None) == INVALID
+    assert pa._lib.pot_norm_rope(ctypes.byref(pa.make_rope()), 1, None, 2, 0.0, None, None, 1, 1, 1, 1, 2, None) == INVALID
 
 
 def test_binding_refuses_tensors_that_do_not_go_together():
