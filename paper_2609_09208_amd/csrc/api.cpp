@@ -152,7 +152,14 @@ int device_cus() {
 //    waves claim tiles (512 units, T = 16384 205 against 208), in three splits where
 //    those make at most four rounds instead of two whole ones (T = 16384, 320 units
 //    145 against 159 with one; 352 units, a fifth round, 168 against 162).
-constexpr int kShortKeys = 768, kLongKeys = 8192, kSpreadKeys = 12288;
+//  - A length per sequence (4-bit values), up to one unit per CU and at least 1000 keys a
+//    split: four four-wave workgroups to a CU, so that the CUs that short sequences leave
+//    early are filled from the longer ones. Sequences of T down to T/B keys, us, here and by
+//    the rules above: 32 units T = 32768 17.1 and 19.6, 64 units T = 16384 17.3 and 20.2
+//    (PoT-M1 19.3 and 23.4; all of T keys 23.2 and 22.0), T = 8192 (512 keys) 14.5 and 14.2,
+//    96 units T = 16384 PoT-M4 30.5 and 45.8, 160 units T = 8192 20.3 and 26.4, 256 units T =
+//    16384 39.6 and 45.9, T = 4096 18.6 and 17.8; 400 units T = 16384 59.4 and 50.2.
+constexpr int kShortKeys = 768, kLongKeys = 8192, kSpreadKeys = 12288, kRaggedKeys = 1000;
 struct Launch {
   Plan plan;
   bool pool;
@@ -179,6 +186,7 @@ struct PlanEngine {
   int pw;            // waves of its CU-wide workgroups, 0: none
   bool int8_values;
   bool light;        // PoT-4 or INT8 keys over fp16 values: the stream decides even on one CU
+  bool ragged;       // a length per sequence
 };
 
 Launch plan_launch(long units, int T, const PlanEngine& e, int cus, int bound) {
@@ -186,6 +194,10 @@ Launch plan_launch(long units, int T, const PlanEngine& e, int cus, int bound) {
   const bool one_tile = pw > 0 && (T <= kShortKeys || (T <= pw * 64 && 4 * units >= cus));
   int S = 1;
   bool pool = pw > 0;
+  if (e.ragged && units <= cus) {
+    const long S4 = 4L * cus / units;
+    if (T >= kRaggedKeys * S4) return {plan_from_count(T, (int)std::min(S4, (long)bound)), false};
+  }
   if (units <= cus) {
     if (!one_tile) S = (int)(cus / units);
     if (S == 1 && T >= kSpreadKeys) {
@@ -319,7 +331,7 @@ pot_status decode_common(int mode, int mant_bits, DecodeArgs& a, const int32_t* 
     pool = pw > 0 && want != kBlock / 64 && (want == pw || units * p.n_splits <= cus);
   } else {
     const PlanEngine e{want == kBlock / 64 ? 0 : pw, v8,
-                       mbits == 0 && mode != kScoreFp16 && !v8};
+                       mbits == 0 && mode != kScoreFp16 && !v8, a.seq_lens != nullptr};
     const Launch l = plan_launch(units, T, e, cus, plan_bound(B, Hkv, T).n_splits);
     p = l.plan;
     pool = pw > 0 && (want == pw || l.pool);

@@ -220,6 +220,20 @@ def test_full_chip_claims_tiles():
         _check(one, ragged[b:b + 1], lens[b:b + 1])
 
 
+def test_long_ragged_batch_as_planned():
+    """From 1000 keys a split on, sequences with lengths of their own are cut into more, smaller workgroups."""
+    B, T = 16, 16001
+    c = _case(13, B, 4, 4, T, 0)
+    dev = _dev(c)
+    lens = np.array([T - b * T // B for b in range(B - 1)] + [0], np.int32)
+    dbg = _run(c, dev, to_dev(lens))
+    assert dbg.wg_waves == 4 and dbg.n_splits > 4
+    _check(c, dev["out"].cpu().numpy(), lens)
+    dbg = _run(c, dev)
+    assert dbg.wg_waves > 4
+    _check(c, dev["out"].cpu().numpy())
+
+
 def test_graph_replays_and_streams():
     """An append with lengths, captured: replays with other lengths and queries equal the eager calls; two streams with
     a workspace each do too."""
