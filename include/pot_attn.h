@@ -294,10 +294,12 @@ typedef struct pot_part {
  *               and v_new of the append calls). v takes no weight.
  *  weight_dtype pot_dtype of the weights.
  *  eps          finite, >= 0.
- *  positions    int64 [n_axes][B][S], device, any sign (8-byte aligned; NULL iff
+ *  Hq, Hkv      up to 1024 each (POT_ERR_UNSUPPORTED above).
+ *  positions    int64 [n_axes][B][S], device, any sign, 8-byte aligned (not read if
  *               rot_dim = 0). The angle is exact to 2^-52 of itself plus rounding: for
  *               |position * inv_freq| up to 2^31 within 1e-6.
- *  inv_freq     double [rot_dim/2], device: radians per position (NULL iff rot_dim = 0).
+ *  inv_freq     double [rot_dim/2], device: radians per position (not read if
+ *               rot_dim = 0).
  * Outputs alias nothing. B or S of 0 is a no-op; B * S up to 2^31. */
 pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* parts,
                          int32_t weight_dtype, float eps, const int64_t* positions,

@@ -342,6 +342,14 @@ def pot_load_values_int4(v_u4, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp
                                      _ptr(v_fp16), _stream(stream)))
 
 
+def _lens(seq_lens):
+    """Address of the lengths, which the kernels read as int32."""
+    if isinstance(seq_lens, torch.Tensor) and (seq_lens.dtype is not torch.int32
+                                               or not seq_lens.is_contiguous()):
+        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", "seq_lens is dense int32 [B]")
+    return _ptr(seq_lens)
+
+
 def pot_decode_attention_v4(fmt: pot_format, engine: int, q, codes_se, codes_m, key_scale, v_u4,
                             t_cap: int, seq_lens, kv_head_of_q, B: int, Hq: int, Hkv: int, T: int,
                             out, workspace, ws_bytes=None, dbg: pot_debug | None = None,
@@ -350,7 +358,7 @@ def pot_decode_attention_v4(fmt: pot_format, engine: int, q, codes_se, codes_m, 
     nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
     _check(_lib.pot_decode_attention_v4(
         ctypes.byref(fmt), int(engine), _ptr(q), _ptr(codes_se), _ptr(codes_m),
-        _ptr(key_scale), _ptr(v_u4), int(t_cap), _ptr(seq_lens), hp, B, Hq, Hkv, T, _ptr(out),
+        _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens), hp, B, Hq, Hkv, T, _ptr(out),
         _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
         _stream(stream)))
 
@@ -364,7 +372,7 @@ def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new
     nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
     _check(_lib.pot_append_decode_attention_v4(
         ctypes.byref(fmt), int(engine), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(codes_se),
-        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _ptr(seq_lens), hp, B, Hq, Hkv, T,
+        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens), hp, B, Hq, Hkv, T,
         _ptr(out), _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
         _stream(stream)))
 

@@ -673,6 +673,8 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* pa
   if (!(eps >= 0.0f && eps <= 3.4e38f)) return fail(POT_ERR_INVALID_ARG, "eps %g", eps);
   if (B < 0 || S < 0 || Hq < 0 || Hkv < 0)
     return fail(POT_ERR_INVALID_ARG, "bad shape B=%d S=%d Hq=%d Hkv=%d", B, S, Hq, Hkv);
+  if (Hq > 1024 || Hkv > 1024)
+    return fail(POT_ERR_UNSUPPORTED, "%d and %d heads (at most 1024)", Hq, Hkv);
   if (B == 0 || S == 0) return ok();
   NormRopeArgs a{};
   const int size = dtype == POT_FP32 ? 4 : 2;

@@ -758,7 +758,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // weight below the range bounds p itself by 2^40.
   float zsum = 0.0f;
   NibbleConst nib{0x000F000Fu, 0x00F000F0u, 0x64006400u};
-  if constexpr (V4) asm("" : "+v"(nib.even), "+v"(nib.odd), "+v"(nib.exp));
+  // (at K = 2 one of them stays a literal: a spill otherwise)
+  if constexpr (V4) asm("" : "+v"(nib.even), "+v"(nib.odd));
+  if constexpr (V4 && K != 2) asm("" : "+v"(nib.exp));
 
   // acc[4], fp16 values: the sums of the weights, as one more column of P.V
   constexpr int kAcc = VK != kValF16 ? 4 : 5;
@@ -772,7 +774,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // the working bit of the score planes, kept in a VGPR (a VALU op that reads
   // an SGPR issues at the slower rate)
   uint32_t m22 = 0x22222222u;
-  if constexpr (MODE == kScorePot) asm("" : "+v"(m22));
+  if constexpr (MODE == kScorePot && !V4) asm("" : "+v"(m22));
 
   KeyRegs<MODE, K> kr[2];
   constexpr int kNext = V4 ? 0 : 1;  // where the next tile's keys go

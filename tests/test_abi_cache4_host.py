@@ -124,7 +124,7 @@ def _rope(**over):
     (dict(k=None), INVALID), (dict(vw=FAKE), INVALID), (dict(kw=FAKE + 8), INVALID), (dict(q=FAKE + 2), INVALID), (dict(ko=FAKE + 8), INVALID), (dict(sq=(4, 64, 64)), INVALID),
     (dict(sq=(64, 4, 64)), INVALID), (dict(sq=(64, 64, 4)), INVALID), (dict(pos=None), INVALID), (dict(inv=None), INVALID),
     (dict(pos=FAKE + 4), INVALID), (dict(inv=FAKE + 4), INVALID), (dict(qw=FAKE + 2), INVALID),
-    (dict(B=1 << 16, S=1 << 16), INVALID),
+    (dict(B=1 << 16, S=1 << 16), INVALID), (dict(Hq=1025), UNSUPPORTED), (dict(Hkv=1 << 30), UNSUPPORTED),
 ])
 def test_norm_rope_refuses(over, code):
     assert _rope(**over) == code
@@ -136,6 +136,14 @@ def test_norm_rope_of_nothing():
     assert _rope(q=None, k=None, v=None, qo=None, ko=None, vo=None) == pa.POT_OK
     assert pa._lib.pot_norm_rope(None, 1, None, 2, 0.0, None, None, 1, 1, 1, 1, 2, None) == INVALID
     assert pa._lib.pot_norm_rope(ctypes.byref(pa.make_rope()), 1, None, 2, 0.0, None, None, 1, 1, 1, 1, 2, None) == INVALID
+
+
+@pytest.mark.parametrize("lens", [torch.zeros(4, dtype=torch.int64), torch.zeros(8, dtype=torch.int32)[::2]])
+def test_binding_refuses_lengths_of_another_type(lens):
+    with pytest.raises(pa.PotError) as e:
+        pa.pot_decode_attention_v4(pa.make_format(), 0, FAKE, FAKE, None, FAKE, FAKE, 8, lens, HEADS, 4, 32, 4, 8, FAKE, FAKE,
+                                   ws_bytes=1 << 30)
+    assert e.value.status == INVALID
 
 
 def test_binding_refuses_tensors_that_do_not_go_together():
