@@ -774,7 +774,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // the working bit of the score planes, kept in a VGPR (a VALU op that reads
   // an SGPR issues at the slower rate)
   uint32_t m22 = 0x22222222u;
-  if constexpr (MODE == kScorePot && !V4) asm("" : "+v"(m22));
+  if constexpr (MODE == kScorePot) asm("" : "+v"(m22));
 
   KeyRegs<MODE, K> kr[2];
   constexpr int kNext = V4 ? 0 : 1;  // where the next tile's keys go
