@@ -300,7 +300,7 @@ typedef struct pot_part {
  *               |position * inv_freq| up to 2^31 within 1e-6.
  *  inv_freq     double [rot_dim/2], device: radians per position (not read if
  *               rot_dim = 0).
- * Outputs alias nothing. B or S of 0 is a no-op; B * S up to 2^31. */
+ * Outputs alias nothing. B or S of 0 is a no-op; B * S up to 2^28. */
 pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* parts,
                          int32_t weight_dtype, float eps, const int64_t* positions,
                          const double* inv_freq, int32_t B, int32_t S, int32_t Hq, int32_t Hkv,

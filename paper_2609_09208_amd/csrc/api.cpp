@@ -688,7 +688,7 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* pa
     return fail(POT_ERR_INVALID_ARG, "positions or inv_freq is NULL");
   if (!aligned(positions, 8) || !aligned(inv_freq, 8))
     return fail(POT_ERR_INVALID_ARG, "positions and inv_freq must be 8-byte aligned");
-  if ((int64_t)B * S > ((int64_t)1 << 31))
+  if ((int64_t)B * S > ((int64_t)1 << 28))  // 2^31 work-items, of 2^32 that a dispatch holds
     return fail(POT_ERR_INVALID_ARG, "B * S too large");
   a.q_weight = a.q.data ? parts[0].weight : nullptr;
   a.k_weight = a.k.data ? parts[1].weight : nullptr;

@@ -131,6 +131,11 @@ def test_norm_rope_refuses(over, code):
     assert pa.pot_last_error() != ""
 
 
+def test_norm_rope_refuses_more_tokens_than_a_dispatch_holds():
+    assert _rope(B=1 << 14, S=1 << 15) == INVALID
+    assert "too large" in pa.pot_last_error()
+
+
 def test_norm_rope_of_nothing():
     assert _rope(B=0) == pa.POT_OK and _rope(S=0) == pa.POT_OK
     assert _rope(q=None, k=None, v=None, qo=None, ko=None, vo=None) == pa.POT_OK
