@@ -64,6 +64,7 @@ class pot_part(ctypes.Structure):
 
 POT_FP16, POT_BF16, POT_FP32 = 0, 1, 2
 POT_INT4_GROUP_BYTES = 288
+POT_MAX_AXES = 4
 
 
 def make_rope(rot_dim: int = HEAD_DIM, neighbours: bool = False, axis_of_pair=None,
@@ -71,6 +72,9 @@ def make_rope(rot_dim: int = HEAD_DIM, neighbours: bool = False, axis_of_pair=No
     """Rotation of a head's first rot_dim elements; axis_of_pair: the position axis of
     each of its rot_dim/2 pairs (None: one axis)."""
     axes = [0] * (rot_dim // 2) if axis_of_pair is None else [int(a) for a in axis_of_pair]
+    if len(axes) != rot_dim // 2 or not all(0 <= a < POT_MAX_AXES for a in axes):
+        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG",
+                       "axis_of_pair: one axis, 0 to 3, for each of the rot_dim / 2 pairs")
     return pot_rope(head_dim, rot_dim, int(bool(neighbours)), max(axes, default=0) + 1,
                     (ctypes.c_uint8 * 32)(*axes))
 
@@ -342,10 +346,11 @@ def pot_load_values_int4(v_u4, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp
                                      _ptr(v_fp16), _stream(stream)))
 
 
-def _lens(seq_lens):
+def _lens(seq_lens, B: int):
     """Address of the lengths, which the kernels read as int32."""
     if isinstance(seq_lens, torch.Tensor) and (seq_lens.dtype is not torch.int32
-                                               or not seq_lens.is_contiguous()):
+                                               or not seq_lens.is_contiguous()
+                                               or seq_lens.numel() < B):
         raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", "seq_lens is dense int32 [B]")
     return _ptr(seq_lens)
 
@@ -358,7 +363,7 @@ def pot_decode_attention_v4(fmt: pot_format, engine: int, q, codes_se, codes_m, 
     nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
     _check(_lib.pot_decode_attention_v4(
         ctypes.byref(fmt), int(engine), _ptr(q), _ptr(codes_se), _ptr(codes_m),
-        _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens), hp, B, Hq, Hkv, T, _ptr(out),
+        _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens, B), hp, B, Hq, Hkv, T, _ptr(out),
         _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
         _stream(stream)))
 
@@ -372,7 +377,7 @@ def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new
     nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
     _check(_lib.pot_append_decode_attention_v4(
         ctypes.byref(fmt), int(engine), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(codes_se),
-        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens), hp, B, Hq, Hkv, T,
+        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens, B), hp, B, Hq, Hkv, T,
         _ptr(out), _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
         _stream(stream)))
 

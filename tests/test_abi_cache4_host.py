@@ -151,6 +151,21 @@ def test_binding_refuses_lengths_of_another_type(lens):
     assert e.value.status == INVALID
 
 
+def test_binding_refuses_too_few_lengths():
+    with pytest.raises(pa.PotError) as e:
+        pa.pot_decode_attention_v4(pa.make_format(), 0, FAKE, FAKE, None, FAKE, FAKE, 8, torch.zeros(3, dtype=torch.int32), HEADS,
+                                   4, 32, 4, 8, FAKE, FAKE, ws_bytes=1 << 30)
+    assert e.value.status == INVALID
+
+
+@pytest.mark.parametrize("rot_dim,axes", [(64, [0] * 31), (64, [0] * 33), (32, [0] * 32), (64, [0] * 31 + [4]), (64, [-1] * 32),
+                                          (64, [256] * 32), (8, [])])
+def test_binding_refuses_axes_that_are_not_one_a_pair(rot_dim, axes):
+    with pytest.raises(pa.PotError) as e:
+        pa.make_rope(rot_dim, axis_of_pair=axes)
+    assert e.value.status == INVALID
+
+
 def test_binding_refuses_tensors_that_do_not_go_together():
     x = torch.zeros((2, 3, 4, 64))
     out = torch.zeros((2, 4, 3, 64))
