@@ -122,8 +122,9 @@ struct DecodeArgs {
 // none: four SIMDs times the waves per SIMD that the kernel's registers
 // allow (512 per lane and SIMD): the shift-accumulate kernels 4 at k <= 2
 // and 3 at k = 3, 4 (fp16 or INT8 values); the decoded-code engines 4, or 3
-// for PoT-4 bytes over fp16 values or with power-of-two weights; the INT8
-// comparator 3. The fp16 comparator has none: with 12 waves it was no faster on
+// for PoT-4 bytes over fp16 values or with power-of-two weights (4-bit values as
+// the others: 16 waves at k = 3, 4 were equal at B = 64 and 1 us of 33 slower at
+// B = 8); the INT8 comparator 3. The fp16 comparator has none: with 12 waves it was no faster on
 // long ranges (graph replays, us: 256 units T = 32768 322 against 323 on four
 // waves, 64 units 86.2 and 85.8, 4 units 13.2 and 12.3).
 constexpr int pool_waves(int mode, int mant_bits, int vf) {
@@ -146,7 +147,8 @@ constexpr int query_words(int G) { return (33 * G + 63) / 64 * 64; }
 
 // vf: value format. 0: fp16 value cache (a.v); 1: INT8 value cache (a.v8,
 // a.v_exp); 2: INT8 values with the power-of-two weights of eq. logsm; 3: values
-// in 4 bits (a.v4, a.seq_lens; no debug taps). Formats 1 to 3 exist for the score modes kScorePot and kScoreDs4a only.
+// in 4 bits (a.v4, a.seq_lens; no debug taps). Formats 1 to 3 exist for the
+// score modes kScorePot and kScoreDs4a only.
 // ev_begin / ev_end (may be null) are recorded on the stream right before and
 // right after the decode kernel.
 hipError_t launch_decode(int mode, int G, int mant_bits, bool debug, int vf,
