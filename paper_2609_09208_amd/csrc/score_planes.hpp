@@ -182,8 +182,8 @@ __device__ __forceinline__ f32x4 score_set(const uint32_t (&w)[4], const uint32_
 // 2 (k + 1) operands instead of the 7 + k of one bit position each, and still no value that
 // is not a power of two. 8 matrix instructions of a tile's scores instead of 28 at k = 0, 16
 // instead of 32 at k = 1, 24 instead of 36 at k = 2, 32 instead of 40 at k = 3 and 40
-// instead of 44 at k = 4. With 4-bit values the matrix cores' power decides how long a full chip takes: B
-// = 64, T = 32768, PoT-4 161 us with a ternary operand per position.
+// instead of 44 at k = 4. With 4-bit values the matrix cores' power decides how long a full
+// chip takes: B = 64, T = 32768, PoT-4 161 us with a ternary operand per position.
 //
 // The operand nibbles are looked up, four at a time, by v_perm_b32: those of even elements
 // in bytes' low halves, of odd ones from the same table four bits up.
