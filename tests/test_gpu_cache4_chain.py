@@ -127,3 +127,53 @@ def test_a_captured_step_follows_its_inputs():
         torch.cuda.synchronize()
         assert torch.equal(layer.out, eager.out), i
         assert torch.equal(layer.v4, eager.v4) and torch.equal(layer.cache["codes_se"], eager.cache["codes_se"])
+
+
+def test_bulk_calls_on_another_stream_and_captured():
+    n, cap = 1029, 1032
+    fmt, heads = pa.make_format(1, hadamard=True), B * HKV
+    one = Layer(1, True)
+    x = torch.empty((B, n, HQ + 2 * HKV, 64), dtype=torch.bfloat16, device=DEV)
+    pos = torch.empty((3, B, n), dtype=torch.int64, device=DEV)
+    cache, v4 = pa.alloc_pot_cache(B, HKV, cap, 1, DEV), pa.alloc_value_cache_int4(B, HKV, cap, DEV)
+    q = torch.empty((B, HQ, n, 64), dtype=torch.bfloat16, device=DEV)
+    k, v, k_back, v_back = (torch.empty((B, HKV, n, 64), dtype=torch.float16, device=DEV) for _ in range(4))
+    codes = cache["codes_se"], cache["codes_m"], cache["key_scale"]
+
+    def layer():
+        one._rows(x, pos, q, k, v)
+        for s in range(heads):
+            b, h = divmod(s, HKV)
+            pa.pot_encode_keys(fmt, k[b, h], n, 1, 0, cache["key_scale"][b, h], cache["codes_se"][b, h], cache["codes_m"][b, h])
+        pa.pot_store_values_int4(v, heads, n, cap, 0, v4)
+        pa.pot_load_keys(fmt, *codes, heads, n, cap, 0, k_back)
+        pa.pot_load_values_int4(v4, heads, n, cap, 0, v_back)
+
+    def fill(seed):
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        pos.copy_(_positions(100 * seed, n))
+
+    side = torch.cuda.Stream()
+    results = []
+    for seed in range(3):  # eager, on a stream of its own
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            fill(seed)
+            layer()
+        torch.cuda.current_stream().wait_stream(side)
+        results.append([t.clone() for t in (q, k, v, k_back, v_back)])
+    torch.cuda.synchronize()
+    assert not torch.equal(results[0][3], results[1][3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer()
+    for seed in (1, 0, 2, 2):
+        fill(seed)
+        for t in (q, k, v, k_back, v_back):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip((q, k, v, k_back, v_back), results[seed]):
+            assert torch.equal(got, want), seed
