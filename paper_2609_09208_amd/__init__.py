@@ -383,8 +383,8 @@ def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new
 
 
 _DTYPES = {torch.float16: POT_FP16, torch.bfloat16: POT_BF16, torch.float32: POT_FP32}
-_pack_parts = struct.Struct("18q").pack  # three pot_part
-_NO_PART = (0, 0, 0, 0, 0, 0)
+_pack_part = struct.Struct("6q").pack  # a pot_part
+_NO_PART = bytes(48)
 
 
 def _mismatch(what: str):
@@ -392,9 +392,8 @@ def _mismatch(what: str):
 
 
 def _part(x, weight, out, B: int, S: int, dtype, out_type):
-    """The fields of pot_part of a projection's rows [B, S, heads, 64] (any strides, elements
-    side by side) whose output is dense [B, heads, S, 64] (of out_type, if given), and its
-    heads."""
+    """pot_part of a projection's rows [B, S, heads, 64] (any strides, elements side by side)
+    whose output is dense [B, heads, S, 64] (of out_type, if given), and its heads."""
     b, s, h, d = x.shape
     sb, ss, sh, se = x.stride()
     if b != B or s != S or d != HEAD_DIM or se != 1 or x.dtype is not dtype:
@@ -408,7 +407,7 @@ def _part(x, weight, out, B: int, S: int, dtype, out_type):
         if weight.numel() != HEAD_DIM or not weight.is_contiguous():
             _mismatch("weights are [64] and dense")
         w = weight.data_ptr()
-    return h, x.data_ptr(), sb, ss, sh, w, out.data_ptr()
+    return h, _pack_part(x.data_ptr(), sb, ss, sh, w, out.data_ptr())
 
 
 def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions, inv_freq,
@@ -422,28 +421,36 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
         return
     B, S, _, _ = first.shape
     dtype, types = first.dtype, _DTYPES
-    hq, *at_q = (0, *_NO_PART) if q is None else _part(q, q_weight, q_out, B, S, dtype, None)
-    hk, *at_k = (0, *_NO_PART) if k is None else _part(k, k_weight, k_out, B, S, dtype,
-                                                       torch.float16)
-    hv, *at_v = (0, *_NO_PART) if v is None else _part(v, None, v_out, B, S, dtype, torch.float16)
+    hq = hk = hv = 0
+    part_q = part_k = part_v = _NO_PART
+    if q is not None:
+        hq, part_q = _part(q, q_weight, q_out, B, S, dtype, None)
+    if k is not None:
+        hk, part_k = _part(k, k_weight, k_out, B, S, dtype, torch.float16)
+    if v is not None:
+        hv, part_v = _part(v, None, v_out, B, S, dtype, torch.float16)
     if hk and hv and hk != hv:
         _mismatch("k and v have the same number of heads")
     w = q_weight if q_weight is not None else k_weight
     if k_weight is not None and k_weight.dtype is not w.dtype:
         _mismatch("weights are of one type")
-    if positions is not None and (positions.dtype is not torch.int64 or not positions.is_contiguous()
-                                  or positions.numel() != rope.n_axes * B * S):
-        _mismatch("positions are dense int64 [n_axes, B, S]")
-    if inv_freq is not None and (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
-                                 or inv_freq.numel() < rope.rot_dim // 2):
-        _mismatch("inv_freq is dense float64 [rot_dim / 2]")
+    at = turns = None
+    if positions is not None:
+        if (positions.dtype is not torch.int64 or not positions.is_contiguous()
+                or positions.numel() != rope.n_axes * B * S):
+            _mismatch("positions are dense int64 [n_axes, B, S]")
+        at = positions.data_ptr()
+    if inv_freq is not None:
+        if (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
+                or inv_freq.numel() < rope.rot_dim // 2):
+            _mismatch("inv_freq is dense float64 [rot_dim / 2]")
+        turns = inv_freq.data_ptr()
     qtype = types.get(q_out.dtype) if q_out is not None else POT_FP32
     itype, wtype = types.get(dtype), types.get(w.dtype) if w is not None else POT_FP32
     if qtype is None or itype is None or wtype is None:
         _mismatch("types are float16, bfloat16 or float32")
-    _check(_lib.pot_norm_rope(ctypes.byref(rope), itype, _pack_parts(*at_q, *at_k, *at_v), wtype,
-                              eps, _ptr(positions), _ptr(inv_freq), B, S, hq, hk or hv, qtype,
-                              _stream(stream)))
+    _check(_lib.pot_norm_rope(ctypes.byref(rope), itype, part_q + part_k + part_v, wtype, eps, at,
+                              turns, B, S, hq, hk or hv, qtype, _stream(stream)))
 
 
 def pot_ds4a_decode_attention(fmt: pot_format, q, codes_se, key_scale, v_fp16, t_cap: int,
