@@ -454,7 +454,8 @@ pot_status pot_append_decode_attention_v8(const pot_format* fmt, int32_t engine,
  *    O = sum_t p_t (z_t + s_t n_t) / sum_t p_t
  * with the weights p of pot_decode_attention. The weights p_t s_t go to the matrix
  * cores as fp16 high and low parts, the codes as the fp16 numbers n_t - 8 (exact), sums
- * are fp32; p_t (z_t + 8 s_t) is summed in fp32 beside them.
+ * are fp32; p_t (z_t + 8 s_t) is summed in fp32 beside them. Scores, formed in fp32 in the
+ * log2 domain, may lie anywhere from -2^31 to 2^31.
  *  engine    as pot_decode_attention_v8.
  *  v_u4      [B*Hkv][t_cap/8][POT_INT4_GROUP_BYTES], 16-byte aligned.
  *  seq_lens  device int32 [B], or NULL: sequence b attends over its first

@@ -81,6 +81,10 @@ constexpr float kPScale = 12.0f;  // p is formed as 2^(x - M + 12) (fp16-normal 
 // 4-bit values: weights are formed as 2^(x - R + 8) s and may grow to 2^16 (fp16's range) before
 // the reference R rises.
 constexpr float kPScale4 = 8.0f, kMostWeight4 = 65000.0f;
+// From this reference on (either sign) every tile raises it, with exponents that are exact:
+// fp32's steps there grow to 256, and the multiply-add of the other tiles, whose product is
+// not rounded, would differ from the x that set R by half of one (Inf or NaN from 2^27 on).
+constexpr int kFarReference = 1 << 22;
 constexpr int kDppRowRor8 = 0x128;  // DPP row_ror:8: lane l reads lane l ^ 8 within its row of 16
 
 // max(a, b) for scores (never NaN) as v_max_f32 without operand canonicalisation
@@ -423,6 +427,13 @@ __device__ __forceinline__ float step8_plus(uint32_t s, uint32_t z, bool hi) {
     asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel:[0,0,0] op_sel_hi:[1,0,1]"
         : "=v"(c) : "v"(s), "s"(8.0f), "v"(z));
   return c;
+}
+
+// The largest integer not above x; past int32's range its nearest end.
+__device__ __forceinline__ int floor_to_int(float x) {
+  int i;
+  asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(i) : "v"(x));
+  return i;
 }
 
 // Steps of 0 (constant rows, and keys past the range) as 2^-24, fp16's smallest number.
@@ -909,7 +920,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   int m_new = m_run;
   bool first = true;
   bool tail_tile = false;
-  float bias4 = hvalid ? kPScale4 - (float)INT_MIN : 0.0f;  // 4-bit values: kPScale4 - R
+  float bias4 = 0.0f;  // 4-bit values: kPScale4 - R
+  bool far = true;     // 4-bit values, uniform: a head's reference is far (or not there yet)
   uint32_t hw[4], lw[4];  // the weights' fp16 high and low parts, two keys each
   auto stage1 = [&](const KeyRegs<MODE, K>& ks, KeyRegs<MODE, K>& knext, int jt) {
     const int t0 = t_begin + kWTile * jt;
@@ -1037,16 +1049,20 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     m_run = m_new;
   };
 
-  // 4-bit values: the tile's weights (in hw, lw) and their sums. True if one is out of
-  // range: the reference has to rise, nothing is summed yet.
+  // 4-bit values: the tile's weights (in hw, lw) and their sums. In the hot loop the
+  // exponents are one multiply-add, and true is returned if a weight is out of range: the
+  // reference has to rise, nothing is summed yet. RAISED: raise4 has put the exponents in
+  // xv, and weights are at most 2^8.
   float psum = 0.0f, pzsum = 0.0f;
-  auto weights4 = [&](bool tail, int k0) -> bool {
+  auto weights4 = [&](auto raised, bool tail, int k0) -> bool {
     if constexpr (V4) {
     const uint32_t sw[4] = {vr.s.x, vr.s.y, vr.s.z, vr.s.w};
     const uint32_t zw[4] = {vr.z.x, vr.z.y, vr.z.z, vr.z.w};
     float p[8], w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(xv[i], c_lane, bias4));
+    for (int i = 0; i < 8; ++i)
+      p[i] = __builtin_amdgcn_exp2f(decltype(raised)::value
+                                        ? xv[i] : __builtin_fmaf(xv[i], c_lane, bias4));
     if (tail) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = k0 + i < t_end ? p[i] : 0.0f;
@@ -1075,25 +1091,42 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     }
     return false;
   };
-  // The reference that takes in the tile at hand: above x + log2 s of its keys.
-  auto raised4 = [&](bool tail, int k0) -> int {
+  // Raises the reference to take in the tile at hand: no smaller than x + log2 s of its keys,
+  // and less than 1 above the largest. log2 s is added to differences from the lane's largest
+  // x (beside a large x it would be lost), and xv becomes x - R + 8 of the same rounded x, R
+  // in two parts that fp32 holds.
+  auto raise4 = [&](bool tail, int k0) {
     if constexpr (V4) {
     const uint32_t sw[4] = {vr.s.x, vr.s.y, vr.s.z, vr.s.w};
-    float mx = -INFINITY;
+    float top = -INFINITY, rest = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      xv[i] = __fmul_rn(xv[i], c_lane);
+      if (!tail || k0 + i < t_end) top = fmaxf(top, xv[i]);
+    }
+    top = floorf(top);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float st = (float)__builtin_bit_cast(half2v, sw[i / 2])[i & 1];
-      const float x = __fmul_rn(xv[i], c_lane) + __builtin_amdgcn_logf(st);
-      if (!tail || k0 + i < t_end) mx = fmaxf(mx, x);
+      const float y = (xv[i] - top) + __builtin_amdgcn_logf(st);
+      if (!tail || k0 + i < t_end) rest = fmaxf(rest, y);
     }
-    mx = fmaxf(mx, dpp_move<kDppRowRor8>(mx));
-    int mt = (hvalid && mx > -INFINITY) ? (int)ceilf(mx) : INT_MIN;
+    int mt = hvalid && fabsf(top) < INFINITY
+                 ? __builtin_elementwise_sub_sat(floor_to_int(top), floor_to_int(-rest))
+                 : INT_MIN;
+    mt = max(mt, __builtin_amdgcn_mov_dpp(mt, kDppRowRor8, 0xF, 0xF, true));
     const auto r16 = __builtin_amdgcn_permlane16_swap((uint32_t)mt, (uint32_t)mt, false, false);
     mt = max((int)r16[0], (int)r16[1]);
     const auto r32 = __builtin_amdgcn_permlane32_swap((uint32_t)mt, (uint32_t)mt, false, false);
-    return max(m_run, max((int)r32[0], (int)r32[1]));
+    m_new = max(m_run, max((int)r32[0], (int)r32[1]));
+    rescale();
+    const float high = (float)(m_run & ~255);
+    rest = kPScale4 - (float)(m_run & 255);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) xv[i] = hvalid ? (xv[i] - high) + rest : 0.0f;
+    bias4 = hvalid ? kPScale4 - (float)m_run : 0.0f;
+    far = __any(hvalid && (uint32_t)(m_run + kFarReference) >= 2u * kFarReference);
     }
-    return m_run;
   };
 
   // Stage 2 of a tile: weights from the scores and P.V on the matrix cores.
@@ -1219,9 +1252,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     for (;;) {
       stage1(kr[0], kr[kNext], j);
       if constexpr (V4) {
-        if (tail_tile) break;
+        if (tail_tile || far) break;
         least_steps(vr);
-        if (__any(weights4(false, 0))) break;
+        if (__any(weights4(std::false_type{}, false, 0))) break;
       } else {
         if (__any(m_new != m_run)) break;
       }
@@ -1234,10 +1267,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
       const int k0 = t_begin + kWTile * j + 32 * part + 8 * grp;
       if (tail_tile) mask_steps(k0, t_end, vr);
       least_steps(vr);
-      m_new = raised4(tail_tile, k0);
-      rescale();
-      bias4 = hvalid ? kPScale4 - (float)m_run : 0.0f;
-      weights4(tail_tile, k0);
+      raise4(tail_tile, k0);
+      weights4(std::true_type{}, tail_tile, k0);
     } else {
       rescale();
     }
@@ -1250,6 +1281,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // wave of such a group without tiles has zero sums and factor 0). Rows h and h + 8 of
   // the products (weights' high and low parts) sit in the two halves of the
   // wave and are added on the way to LDS.
+  // 4-bit values: the lane's place made again from the thread's index, which is there in any
+  // case (kept over the tiles it made kernels at k = 1 and 2 spill)
+  int tid_m = tid;
+  if constexpr (V4) asm volatile("" : "+v"(tid_m));
+  const int lane_m = V4 ? tid_m & 63 : lane;
+  const int grp_m = V4 ? lane_m >> 4 : grp, row_m = V4 ? lane_m & 15 : row;
   const int n_act = kPool ? min(NW, (n_tiles + 3) & ~3) : NW;
   if (wave < n_act) {
 #pragma unroll
@@ -1259,10 +1296,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
         const uint32_t v = __float_as_uint(acc[nb][r]);
         const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
         const float sum = __uint_as_float(h[0]) + __uint_as_float(h[1]);
-        if (lane < 32) sm.wo[wave][4 * grp + r][16 * nb + row] = sum;
+        if (lane_m < 32) sm.wo[wave][4 * grp_m + r][16 * nb + row_m] = sum;
       }
   }
-  if (lane < 8) sm.wm[wave][lane] = m_run;
+  if (lane_m < 8) sm.wm[wave][lane_m] = m_run;
   if constexpr (V4) {
     zsum += dpp_move<kDppRowRor8>(zsum);
     const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(zsum), __float_as_uint(zsum),
@@ -1271,7 +1308,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(zsum), __float_as_uint(zsum),
                                                       false, false);
     zsum = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
-    if (lane < 8) sz.z[wave][lane] = zsum;
+    if (lane_m < 8) sz.z[wave][lane_m] = zsum;
   }
   if constexpr (V8 || V4) {
     // sum of the weights over the 8 lanes that formed a head's
@@ -1282,19 +1319,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum),
                                                       false, false);
     lsum = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
-    if (lane < 8) sm.wl[wave][lane] = lsum;
+    if (lane_m < 8) sm.wl[wave][lane_m] = lsum;
   } else {
-    // rows 4 grp + r, the same in every column: column r hands over row r
-    const float sum = row == 0 ? acc[4][0] : row == 1 ? acc[4][1] : row == 2 ? acc[4][2] : acc[4][3];
+    // rows 4 grp_m + r, the same in every column: column r hands over row r
+    const float sum = row_m == 0 ? acc[4][0] : row_m == 1 ? acc[4][1] : row_m == 2 ? acc[4][2] : acc[4][3];
     const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum),
                                                     false, false);
-    if (lane < 32 && row < 4)
-      sm.wl[wave][4 * grp + row] = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+    if (lane_m < 32 && row_m < 4)
+      sm.wl[wave][4 * grp_m + row_m] = __uint_as_float(h[0]) + __uint_as_float(h[1]);
   }
   __syncthreads();
 
   const int Sn = a.n_splits;
-  for (int idx = tid; idx < G * kDim; idx += kBlk) {
+  for (int idx = tid_m; idx < G * kDim; idx += kBlk) {
     const int h = __builtin_amdgcn_readfirstlane(idx / kDim), d = idx % kDim;
     const int64_t bq = (int64_t)b * a.Hq + a.q_head(kvh * G + h);
     // lane w holds wave w's maximum, factor and sum of the head
