@@ -630,6 +630,11 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
 }
 
+// 2^(m - M) of two maxima, which may be further apart than an int32 holds.
+__device__ __forceinline__ float pow2_between(int m, int M) {
+  return __builtin_amdgcn_ldexpf(1.0f, __builtin_elementwise_sub_sat(m, M));
+}
+
 // One head's merge by one wave: lane s holds split s's M_s and l_s, and every
 // lane its dimension of all splits' sums, N >= Sn of them requested together
 // (loads in a loop or behind branches wait for each other: 0.6 us a turn).
@@ -648,7 +653,7 @@ __device__ __forceinline__ void merge_head(const DecodeArgs& a, int64_t bq, int 
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = load_agent(po + min(i, Sn - 1) * kDim);
   const int M = wave_max_i32(m_l);
-  const float f_l = lane < Sn && m_l != INT_MIN ? __builtin_amdgcn_ldexpf(1.0f, m_l - M) : 0.0f;
+  const float f_l = lane < Sn && m_l != INT_MIN ? pow2_between(m_l, M) : 0.0f;
   const float l = wave_sum(f_l * l_l);
   float o = 0.0f;
 #pragma unroll
@@ -1033,7 +1038,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
       m_run = m_new;
       return;
     }
-    const float f = (m_run == INT_MIN) ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, m_run - m_new);
+    const float f = (m_run == INT_MIN) ? 0.0f : pow2_between(m_run, m_new);
     const int arow = lane & 15, acol = lane >> 4;
 #pragma unroll
     for (int nb = 0; nb < kAcc; ++nb) {
@@ -1139,12 +1144,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     // at the end, so both blocks see hi + lo of every weight.
     if constexpr (!V4) {
     const float bias = hvalid ? kPScale - (float)m_run : 0.0f;
+    const int m_pow2 = __builtin_elementwise_sub_sat(m_run, (int)kPScale);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float p0, p1;
       if constexpr (kPow2) {
         // A~ = 2^-k with k = M - ceil(x - 1/2) (M - x rounded half up):
-        // p = 2^(ceil(x - 1/2) - M + 12), exact; keys masked to -inf get 0.
+        // p = 2^(ceil(x - 1/2) - (M - 12)), exact; keys masked to -inf get 0.
         // ceil(x - 1/2) is ceil(x), less one when ceil(x) - x >= 1/2: that
         // difference is exact in fp32 where it decides (x - 1/2 itself is
         // not: -0.5 + 2^-25 would round to -1)
@@ -1152,7 +1158,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
           const float c = ceilf(x);
           const float r = (c - x >= 0.5f) ? c - 1.0f : c;
           return x > -INFINITY
-                     ? __builtin_amdgcn_ldexpf(1.0f, (int)r - m_run + (int)kPScale)
+                     ? __builtin_amdgcn_ldexpf(1.0f, __builtin_elementwise_sub_sat((int)r, m_pow2))
                      : 0.0f;
         };
         p0 = pw(xv[2 * i]);
@@ -1339,7 +1345,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     const int m_w = lane < NW ? sm.wm[lane < NW ? lane : 0][h] : INT_MIN;
     const float l_w = lane < NW ? sm.wl[lane < NW ? lane : 0][h] : 0.0f;
     const int M = wave_max_i32(m_w);
-    const float f_w = m_w == INT_MIN ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, m_w - M);
+    const float f_w = m_w == INT_MIN ? 0.0f : pow2_between(m_w, M);
     const float l = wave_sum(f_w * l_w);
     float o = 0.0f;
 #pragma unroll
@@ -1428,7 +1434,7 @@ __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const Decod
     __syncthreads();
     M = max(max(smax[0], smax[1]), max(smax[2], smax[3]));
     const float f_l = valid && !(EMPTY && m_l == INT_MIN)
-                          ? __builtin_amdgcn_ldexpf(1.0f, m_l - M) : 0.0f;
+                          ? pow2_between(m_l, M) : 0.0f;
     float fl = f_l * l_l;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) fl += __shfl_xor(fl, o, 64);
@@ -1449,7 +1455,7 @@ __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const Decod
     M = max(max(smax[0], smax[1]), max(smax[2], smax[3]));
 #pragma unroll 8
     for (int s = w; s < Sn; s += kCombineWaves) {
-      const float f = EMPTY && pm[s] == INT_MIN ? 0.0f : __builtin_amdgcn_ldexpf(1.0f, pm[s] - M);
+      const float f = EMPTY && pm[s] == INT_MIN ? 0.0f : pow2_between(pm[s], M);
       L = fmaf(f, pl[s], L);
       O = fmaf(f, po[s * kDim + d], O);
     }
