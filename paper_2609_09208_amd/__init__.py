@@ -157,12 +157,18 @@ def _check(status: int) -> None:
         raise PotError(status, name, _lib.pot_last_error().decode())
 
 
+def _mismatch(what: str):
+    raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", what)
+
+
 def _ptr(t) -> int | None:
-    """Device pointer of a torch tensor, an int address, or None."""
+    """Address of a tensor on the GPU, an int address, or None."""
     if t is None:
         return None
     if isinstance(t, int):
         return t
+    if not t.is_cuda:  # the kernels would read the host's address
+        _mismatch("tensors on the GPU are needed")
     return t.data_ptr()
 
 
@@ -174,21 +180,32 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
-def _stream(stream) -> int | None:
+def _stream(stream, device=None) -> int | None:
+    """Address of the stream; without one the current stream of the current device, which has
+    to be the call's, if that is given."""
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
-        return _raw_stream(_raw_device())
+    if _raw_stream is not None and _raw_device is not None and (
+            device is not None or torch.cuda.is_initialized()):
+        current = _raw_device()
+        if device is not None and device != current:
+            _mismatch("tensors on the current device are needed")
+        return _raw_stream(current)
     if not torch.cuda.is_available():
         return None
     return torch.cuda.current_stream().cuda_stream
+
+
+def _device(t) -> int | None:
+    """Device of a tensor on the GPU, None of an address."""
+    return t.get_device() if type(t) is torch.Tensor else None
 
 
 def _heads(kv_head_of_q):
     if not (type(kv_head_of_q) is np.ndarray and kv_head_of_q.dtype == np.int32
             and kv_head_of_q.flags.c_contiguous):
         kv_head_of_q = np.ascontiguousarray(kv_head_of_q, dtype=np.int32)
-    return kv_head_of_q, kv_head_of_q.ctypes.data
+    return kv_head_of_q, kv_head_of_q.__array_interface__["data"][0]
 
 
 # ---- C ABI mirrors ---------------------------------------------------------
@@ -318,32 +335,32 @@ def pot_append_decode_attention_v8(fmt: pot_format, engine: int, q, k_new, v_new
 def pot_store_values_int4(v_fp16, n_seq: int, n_tok: int, t_cap: int, t0: int, v_u4,
                           stream=None) -> None:
     _check(_lib.pot_store_values_int4(_ptr(v_fp16), int(n_seq), int(n_tok), int(t_cap),
-                                      int(t0), _ptr(v_u4), _stream(stream)))
+                                      int(t0), _ptr(v_u4), _stream(stream, _device(v_u4))))
 
 
 def pot_load_keys(fmt: pot_format, codes_se, codes_m, key_scale, n_seq: int, n_tok: int,
                   t_cap: int, t0: int, k_fp16, stream=None) -> None:
     _check(_lib.pot_load_keys(ctypes.byref(fmt), _ptr(codes_se), _ptr(codes_m), _ptr(key_scale),
                               int(n_seq), int(n_tok), int(t_cap), int(t0), _ptr(k_fp16),
-                              _stream(stream)))
+                              _stream(stream, _device(k_fp16))))
 
 
 def pot_load_values(v_cache, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp16,
                     stream=None) -> None:
     _check(_lib.pot_load_values(_ptr(v_cache), int(n_seq), int(n_tok), int(t_cap), int(t0),
-                                _ptr(v_fp16), _stream(stream)))
+                                _ptr(v_fp16), _stream(stream, _device(v_fp16))))
 
 
 def pot_load_values_int8(v_u8, v_exp, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp16,
                          stream=None) -> None:
     _check(_lib.pot_load_values_int8(_ptr(v_u8), _ptr(v_exp), int(n_seq), int(n_tok), int(t_cap),
-                                     int(t0), _ptr(v_fp16), _stream(stream)))
+                                     int(t0), _ptr(v_fp16), _stream(stream, _device(v_fp16))))
 
 
 def pot_load_values_int4(v_u4, n_seq: int, n_tok: int, t_cap: int, t0: int, v_fp16,
                          stream=None) -> None:
     _check(_lib.pot_load_values_int4(_ptr(v_u4), int(n_seq), int(n_tok), int(t_cap), int(t0),
-                                     _ptr(v_fp16), _stream(stream)))
+                                     _ptr(v_fp16), _stream(stream, _device(v_fp16))))
 
 
 def _lens(seq_lens, B: int):
@@ -351,7 +368,7 @@ def _lens(seq_lens, B: int):
     if isinstance(seq_lens, torch.Tensor) and (seq_lens.dtype is not torch.int32
                                                or not seq_lens.is_contiguous()
                                                or seq_lens.numel() < B):
-        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", "seq_lens is dense int32 [B]")
+        _mismatch("seq_lens is dense int32 [B]")
     return _ptr(seq_lens)
 
 
@@ -365,7 +382,7 @@ def pot_decode_attention_v4(fmt: pot_format, engine: int, q, codes_se, codes_m, 
         ctypes.byref(fmt), int(engine), _ptr(q), _ptr(codes_se), _ptr(codes_m),
         _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens, B), hp, B, Hq, Hkv, T, _ptr(out),
         _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
-        _stream(stream)))
+        _stream(stream, _device(out))))
 
 
 def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new, codes_se,
@@ -377,9 +394,9 @@ def pot_append_decode_attention_v4(fmt: pot_format, engine: int, q, k_new, v_new
     nbytes = workspace.numel() * workspace.element_size() if ws_bytes is None else ws_bytes
     _check(_lib.pot_append_decode_attention_v4(
         ctypes.byref(fmt), int(engine), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(codes_se),
-        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens, B), hp, B, Hq, Hkv, T,
-        _ptr(out), _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
-        _stream(stream)))
+        _ptr(codes_m), _ptr(key_scale), _ptr(v_u4), int(t_cap), _lens(seq_lens, B), hp, B, Hq, Hkv,
+        T, _ptr(out), _ptr(workspace), nbytes, ctypes.byref(dbg) if dbg is not None else None,
+        _stream(stream, _device(out))))
 
 
 _DTYPES = {torch.float16: POT_FP16, torch.bfloat16: POT_BF16, torch.float32: POT_FP32}
@@ -387,27 +404,28 @@ _pack_part = struct.Struct("6q").pack  # a pot_part
 _NO_PART = bytes(48)
 
 
-def _mismatch(what: str):
-    raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG", what)
-
-
-def _part(x, weight, out, B: int, S: int, dtype, out_type):
-    """pot_part of a projection's rows [B, S, heads, 64] (any strides, elements side by side)
-    whose output is dense [B, heads, S, 64] (of out_type, if given), and its heads."""
+def _part(x, weight, out, tokens, dtype, device, out_type):
+    """(B, S) and heads of a projection's rows [B, S, heads, 64] (any strides, elements side by
+    side; of `tokens`, if given), and their pot_part. The output is dense [B, heads, S, 64] (of
+    out_type, if given)."""
     b, s, h, d = x.shape
     sb, ss, sh, se = x.stride()
-    if b != B or s != S or d != HEAD_DIM or se != 1 or x.dtype is not dtype:
-        _mismatch("rows [B, S, heads, 64] of one type with dense elements are needed")
-    if (out is None or out.numel() != B * h * S * HEAD_DIM or not out.is_contiguous()
+    at = b, s
+    if (d != HEAD_DIM or se != 1 or x.dtype is not dtype or x.get_device() != device
+            or (tokens and at != tokens)):
+        _mismatch("rows [B, S, heads, 64] of one type with dense elements on one GPU are needed")
+    if (out is None or out.numel() != b * s * h * HEAD_DIM or not out.is_contiguous()
+            or out.get_device() != device
             or (out_type is not None and out.dtype is not out_type)):
-        _mismatch("a dense output [B, heads, S, 64] is needed (k and v: float16)")
+        _mismatch("a dense output [B, heads, S, 64] on the rows' GPU is needed (k and v: float16)")
     if weight is None:
         w = 0
     else:
-        if weight.numel() != HEAD_DIM or not weight.is_contiguous():
-            _mismatch("weights are [64] and dense")
+        if (weight.numel() != HEAD_DIM or not weight.is_contiguous()
+                or weight.get_device() != device):
+            _mismatch("weights are [64] and dense, on the rows' GPU")
         w = weight.data_ptr()
-    return h, _pack_part(x.data_ptr(), sb, ss, sh, w, out.data_ptr())
+    return at, h, _pack_part(x.data_ptr(), sb, ss, sh, w, out.data_ptr())
 
 
 def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions, inv_freq,
@@ -419,16 +437,19 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
     first = q if q is not None else k if k is not None else v
     if first is None:
         return
-    B, S, _, _ = first.shape
-    dtype, types = first.dtype, _DTYPES
+    dtype, device, types = first.dtype, first.get_device(), _DTYPES
+    if device < 0:
+        _mismatch("tensors on the GPU are needed")
+    tokens = None
     hq = hk = hv = 0
     part_q = part_k = part_v = _NO_PART
     if q is not None:
-        hq, part_q = _part(q, q_weight, q_out, B, S, dtype, None)
+        tokens, hq, part_q = _part(q, q_weight, q_out, None, dtype, device, None)
     if k is not None:
-        hk, part_k = _part(k, k_weight, k_out, B, S, dtype, torch.float16)
+        tokens, hk, part_k = _part(k, k_weight, k_out, tokens, dtype, device, torch.float16)
     if v is not None:
-        hv, part_v = _part(v, None, v_out, B, S, dtype, torch.float16)
+        tokens, hv, part_v = _part(v, None, v_out, tokens, dtype, device, torch.float16)
+    B, S = tokens
     if hk and hv and hk != hv:
         _mismatch("k and v have the same number of heads")
     w = q_weight if q_weight is not None else k_weight
@@ -437,20 +458,24 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
     at = turns = None
     if positions is not None:
         if (positions.dtype is not torch.int64 or not positions.is_contiguous()
-                or positions.numel() != rope.n_axes * B * S):
-            _mismatch("positions are dense int64 [n_axes, B, S]")
+                or positions.numel() != rope.n_axes * B * S or positions.get_device() != device):
+            _mismatch("positions are dense int64 [n_axes, B, S] on the rows' GPU")
         at = positions.data_ptr()
     if inv_freq is not None:
         if (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
-                or inv_freq.numel() < rope.rot_dim // 2):
-            _mismatch("inv_freq is dense float64 [rot_dim / 2]")
+                or ((n := inv_freq.numel()) < HEAD_DIM // 2 and n < rope.rot_dim // 2)
+                or inv_freq.get_device() != device):
+            _mismatch("inv_freq is dense float64 [rot_dim / 2] on the rows' GPU")
         turns = inv_freq.data_ptr()
+    itype = types.get(dtype)
+    wtype = itype if w is None or w.dtype is dtype else types.get(w.dtype)
     qtype = types.get(q_out.dtype) if q_out is not None else POT_FP32
-    itype, wtype = types.get(dtype), types.get(w.dtype) if w is not None else POT_FP32
     if qtype is None or itype is None or wtype is None:
         _mismatch("types are float16, bfloat16 or float32")
-    _check(_lib.pot_norm_rope(ctypes.byref(rope), itype, part_q + part_k + part_v, wtype, eps, at,
-                              turns, B, S, hq, hk or hv, qtype, _stream(stream)))
+    status = _lib.pot_norm_rope(rope, itype, part_q + part_k + part_v, wtype, eps, at, turns, B, S,
+                                hq, hk or hv, qtype, _stream(stream, device))
+    if status:
+        _check(status)
 
 
 def pot_ds4a_decode_attention(fmt: pot_format, q, codes_se, key_scale, v_fp16, t_cap: int,
