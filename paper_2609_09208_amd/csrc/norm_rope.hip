@@ -144,19 +144,29 @@ __device__ __forceinline__ void load_weights(const void* w, int type, int g, flo
   else to_floats<POT_FP16, MODE>(load_row<POT_FP16, MODE>(w, 0, g), out);
 }
 
-// x / sqrt(mean x^2 + eps) * w over the row's 8 lanes. The hardware's reciprocal root is
-// within a unit in the last place of a normal number; a mean near the smallest ones is
-// scaled first.
-__device__ __forceinline__ void norm_row(float (&x)[8], const float (&w)[8], float eps) {
+// Sum of the squares over the row's 8 lanes.
+__device__ __forceinline__ float row_squares(const float (&x)[8]) {
   float ss = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
   ss += __uint_as_float(lane_xor_u32<1>(__float_as_uint(ss)));
   ss += __uint_as_float(lane_xor_u32<2>(__float_as_uint(ss)));
-  ss += dpp_move<0x141>(ss);  // row_half_mirror: the other half of the 8 lanes
-  const float m = __builtin_fmaf(ss, 1.0f / 64, eps);
-  const bool low = m < 0x1p-96f;
-  const float r = __builtin_amdgcn_rsqf(low ? m * 0x1p96f : m) * (low ? 0x1p48f : 1.0f);
+  return ss + dpp_move<0x141>(ss);  // row_half_mirror: the other half of the 8 lanes
+}
+// x / sqrt(mean x^2 + eps) * w over the row's 8 lanes; every lane of the wave takes part. A row
+// whose squares pass fp32's range, or fall out of it beside a small eps, is first scaled by a
+// power of two. The hardware's reciprocal root is within a unit in the last place.
+__device__ __forceinline__ void norm_row(float (&x)[8], const float (&w)[8], float eps) {
+  float ss = row_squares(x), m = __builtin_fmaf(ss, 1.0f / 64, eps);
+  const bool large = !(ss < 0x1p120f), small = m < 0x1p-80f;
+  if (__any(large || small)) {
+    const float c = large ? 0x1p-70f : small ? 0x1p100f : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= c;
+    ss = row_squares(x);
+    m = __builtin_fmaf(ss, 1.0f / 64, eps * c * c);
+  }
+  const float r = __builtin_amdgcn_rsqf(m);
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
 }
