@@ -452,6 +452,10 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
     B, S = tokens
     if hk and hv and hk != hv:
         _mismatch("k and v have the same number of heads")
+    if q is None:
+        q_weight = None
+    if k is None:
+        k_weight = None
     w = q_weight if q_weight is not None else k_weight
     if k_weight is not None and k_weight.dtype is not w.dtype:
         _mismatch("weights are of one type")

@@ -86,3 +86,21 @@ def test_rows_whose_squares_pass_fp32(tokens, dtype, q_out, rot_dim):
             16 * 2.0 ** -24 + tokens * 2.0 ** -51) + 2.0 ** -133  # bf16's and fp32's smallest numbers
         over = ((out.cpu().double() - want).abs() / bound).nan_to_num(nan=float("inf"))
         assert float(over.max()) <= 1, (eps, float(over.max()))
+
+
+@pytest.mark.parametrize("part", ["q", "k"])
+def test_weights_of_a_part_left_out_are_not_looked_at(part):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    x = torch.randn((1, 5, 3, 64), generator=g, device=DEV).to(torch.bfloat16)
+    w = (1 + 0.2 * torch.randn(64, generator=g, device=DEV)).to(torch.bfloat16)
+    out = torch.empty((1, 3, 5, 64), dtype=torch.float16, device=DEV)
+    pos = torch.arange(5, device=DEV).view(1, 1, 5)
+    for other in (None, w.double(), w.float()):
+        got = torch.zeros_like(out)
+        mine, theirs = (x, w, got), (None, other, None)
+        (q, qw, qo), (k, kw, ko) = (mine, theirs) if part == "q" else (theirs, mine)
+        pa.pot_norm_rope(pa.make_rope(), q, k, None, qw, kw, 1e-6, pos, _inv_freq(64), qo, ko, None)
+        if other is None:
+            out.copy_(got)
+        assert torch.equal(got, out)
