@@ -34,21 +34,19 @@ __device__ __forceinline__ void store_record(const uint4 v, uint8_t* __restrict_
     x[2 * k] = __half2float(__ushort_as_half((unsigned short)(w4[k] & 0xFFFFu)));
     x[2 * k + 1] = __half2float(__ushort_as_half((unsigned short)(w4[k] >> 16)));
   }
-  // the maximum of x and of -x; fmaxf and the median with infinity pass over NaN (the
-  // median does without the canonicalisation that fmaxf's operand from another lane gets)
+  // the maximum of x and of -x over the token's 8 lanes; fmaxf passes over NaN
   float hi = x[0], nlo = -x[0];
 #pragma unroll
   for (int k = 1; k < 8; ++k) {
     hi = fmaxf(hi, x[k]);
     nlo = fmaxf(nlo, -x[k]);
   }
-  constexpr float kInf = __builtin_inff();
-  hi = __builtin_amdgcn_fmed3f(hi, dpp_move<0xB1>(hi), kInf);
-  nlo = __builtin_amdgcn_fmed3f(nlo, dpp_move<0xB1>(nlo), kInf);
-  hi = __builtin_amdgcn_fmed3f(hi, dpp_move<0x4E>(hi), kInf);
-  nlo = __builtin_amdgcn_fmed3f(nlo, dpp_move<0x4E>(nlo), kInf);
-  hi = __builtin_amdgcn_fmed3f(hi, dpp_move<0x141>(hi), kInf);
-  nlo = __builtin_amdgcn_fmed3f(nlo, dpp_move<0x141>(nlo), kInf);
+  hi = fmaxf(hi, dpp_move<0xB1>(hi));
+  nlo = fmaxf(nlo, dpp_move<0xB1>(nlo));
+  hi = fmaxf(hi, dpp_move<0x4E>(hi));
+  nlo = fmaxf(nlo, dpp_move<0x4E>(nlo));
+  hi = fmaxf(hi, dpp_move<0x141>(hi));
+  nlo = fmaxf(nlo, dpp_move<0x141>(nlo));
   // infinite ends are the largest finite numbers; infinite elements then come out as n = 0
   // or 15 by the median below
   const bool any = hi == hi;
