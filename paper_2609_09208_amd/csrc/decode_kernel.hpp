@@ -284,8 +284,8 @@ __device__ __forceinline__ void plane_bits(const KeyRegs<MODE, K>& r, int s, uin
 // whose weights it forms in stage 2.
 // Blocks kFirst .. kEnd - 1 of the two K-blocks; the exponents come with block 0.
 // 4-bit values: one 16-byte load per K-block holds the lane's fragments of all four
-// dimension blocks (pot_device.hpp, value_byte_i4), and the steps and minima of the 8
-// keys whose weights the lane forms stand behind the values of their group.
+// dimension blocks (the record's order in pot_device.hpp), and the steps and minima of the
+// 8 keys whose weights the lane forms stand behind the values of their group.
 template <int VK, int kFirst = 0, int kEnd = 2>
 __device__ __forceinline__ void load_values_buf(const Streams& st, int t0, int lane,
                                                 ValRegs<VK>& v) {

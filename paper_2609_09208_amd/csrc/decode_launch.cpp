@@ -2,10 +2,6 @@
 // translation unit that holds each score mode's kernels.
 #include "pot_launch.hpp"
 
-// Host dispatch of the decode launch to the
-// translation unit that holds each score mode's kernels.
-#include "pot_launch.hpp"
-
 namespace potattn {
 
 hipError_t launch_decode(int mode, int G, int mant_bits, bool debug, int vf,
