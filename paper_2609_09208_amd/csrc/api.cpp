@@ -138,7 +138,8 @@ int device_cus() {
 //    72.2 -> 70.3, 168 75.2 and 77.8). With INT8 values, where a unit takes a CU the
 //    longest, three to four workgroups per CU up to three quarters (132 units 68.0
 //    -> 55.1, 160 69.8 -> 61.2, 176 70.7 -> 66.9, 192 72.8 -> 67.7; T = 8192 38.0 ->
-//    32.5 and 39.6 -> 40.7).
+//    32.5 and 39.6 -> 40.7), and with 4-bit values the same (132 units 46.1 -> 39.2, 160
+//    46.5 -> 42.7, 176 48.3 -> 46.3, 192 49.1 -> 47.9; the best counts 38.1, 42.6, 46.3, 47.5).
 //  - Where every wave of one workgroup has at most one 64-key tile, one split
 //    and no merge: up to 768 keys (T = 512, 4 units 5.8 against 6.8 with two
 //    splits, 64 units 6.1 against 7.2; T = 768, 4 units 6.6 against 6.9 with three;
@@ -152,14 +153,26 @@ int device_cus() {
 //    waves claim tiles (512 units, T = 16384 205 against 208), in three splits where
 //    those make at most four rounds instead of two whole ones (T = 16384, 320 units
 //    145 against 159 with one; 352 units, a fifth round, 168 against 162).
-//  - A length per sequence (4-bit values), up to one unit per CU and at least 1000 keys a
-//    split: four four-wave workgroups to a CU, so that the CUs that short sequences leave
-//    early are filled from the longer ones. Sequences of T down to T/B keys, us, here and by
-//    the rules above: 32 units T = 32768 17.1 and 19.6, 64 units T = 16384 17.3 and 20.2
-//    (PoT-M1 19.3 and 23.4; all of T keys 23.2 and 22.0), T = 8192 (512 keys) 14.5 and 14.2,
-//    96 units T = 16384 PoT-M4 30.5 and 45.8, 160 units T = 8192 20.3 and 26.4, 256 units T =
-//    16384 39.6 and 45.9, T = 4096 18.6 and 17.8; 400 units T = 16384 59.4 and 50.2.
-constexpr int kShortKeys = 768, kLongKeys = 8192, kSpreadKeys = 12288, kRaggedKeys = 1000;
+//  - A length per sequence (4-bit values), up to one unit per CU: four four-wave workgroups
+//    for every CU, from 1000 keys a split and, where one CU-wide workgroup a unit leaves less
+//    than a quarter of the CUs idle, from 1500. They belong to several sequences (four of them
+//    are on a CU at once, three at k = 3 and 4), so that what a short one leaves serves the
+//    others. The lengths are not known here: ones that differ gain, equal ones lose where the
+//    other plan leaves no CU idle. us, here / by the rules above, for lengths from T down to
+//    T/B in equal steps, all T, every other one T/8, all but one T/8:
+//      64 units T = 16384 PoT-4   17.5/19.6  22.9/21.1  21.8/19.3  14.6/18.2
+//      64 units T = 16384 PoT-M4  25.6/28.0  34.0/29.8  30.4/28.5  18.5/26.8
+//      96 units T = 10240 PoT-4   17.1/21.2  22.7/22.2  20.1/21.0  14.6/20.1
+//      160 units T = 6144 PoT-4   17.7/21.5  23.1/22.4  20.8/21.7  14.9/20.3
+//      160 units T = 6144 PoT-M4  26.8/34.9  34.0/35.7  33.0/35.1  17.6/33.8
+//      256 units T = 8192 PoT-4   26.3/27.7  37.4/30.9  34.4/27.8  21.0/24.6
+//    and with fewer keys a split than that:
+//      64 units T = 8192 PoT-4    14.4/13.7  16.8/14.9  16.1/13.7  12.4/12.8
+//      256 units T = 5120 PoT-4   21.5/19.6  27.8/21.6  25.6/20.4  16.7/18.1
+//      256 units T = 4096 PoT-4   19.0/17.7  24.4/19.3  23.0/17.8  15.6/16.4
+//    More units than CUs: 400 units T = 16384 59.4/50.2 in equal steps.
+constexpr int kShortKeys = 768, kLongKeys = 8192, kSpreadKeys = 12288;
+constexpr int kRaggedKeys = 1000, kRaggedKeysFull = 1500;
 struct Launch {
   Plan plan;
   bool pool;
@@ -184,7 +197,7 @@ int spread_splits(long units, long cus) {
 // What of an engine the plan depends on.
 struct PlanEngine {
   int pw;            // waves of its CU-wide workgroups, 0: none
-  bool int8_values;
+  bool int8_values;  // or 4-bit ones
   bool light;        // PoT-4 or INT8 keys over fp16 values: the stream decides even on one CU
   bool ragged;       // a length per sequence
 };
@@ -196,7 +209,7 @@ Launch plan_launch(long units, int T, const PlanEngine& e, int cus, int bound) {
   bool pool = pw > 0;
   if (e.ragged && units <= cus) {
     const long S4 = 4L * cus / units;
-    if (T >= kRaggedKeys * S4) return {plan_from_count(T, (int)std::min(S4, (long)bound)), false};
+    if (T >= (4 * units > 3L * cus ? kRaggedKeysFull : kRaggedKeys) * S4) return {plan_from_count(T, (int)std::min(S4, (long)bound)), false};
   }
   if (units <= cus) {
     if (!one_tile) S = (int)(cus / units);
