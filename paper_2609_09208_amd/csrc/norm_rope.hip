@@ -374,7 +374,11 @@ __global__ __launch_bounds__(64) void norm_rope_heads_kernel(const NormRopeArgs 
   if (__any(kind != 0)) store_row<MODE, false>(out, at, g, POT_FP16, x, there && kind != 0);
 }
 
-// Which kernel: tokens by eights once they fill the chip (see the launch).
+// Which kernel: tokens by eights once the work of the angles, made once a token, is more than
+// the chain through a wave's heads. us, by eights and by heads, bf16: 32 + 4 + 4 heads 512
+// tokens 4.7 and 4.8, 1024 5.2 and 6.6, 2048 7.8 and 10.5, 128 3.9 and 3.5; 8 + 1 + 1 heads 512
+// 3.8 and 3.6, 1024 4.1 and 4.2, 2048 4.7 and 5.7; half of a head turned 512 6.2 and 5.9, 1024
+// 6.8 and 8.5.
 constexpr int64_t kManyTokens = 1024;
 constexpr int64_t kTargetWaves = 4096;
 
@@ -388,7 +392,7 @@ static hipError_t launch_mode(const NormRopeArgs& a, hipStream_t stream) {
                        dim3(64), 0, stream, a, heads, n_groups);
   } else {
     const int64_t groups = (n_tok + 7) / 8;
-    // as many waves as the chip holds at 8 a SIMD, or heads allow
+    // four waves a SIMD, or as many as heads allow
     int64_t n_chunks = (kTargetWaves + groups - 1) / groups;
     n_chunks = n_chunks < heads ? n_chunks : heads;
     const int chunk = (int)((heads + n_chunks - 1) / n_chunks);
