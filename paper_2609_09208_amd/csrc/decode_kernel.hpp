@@ -54,6 +54,7 @@
 #include <climits>
 #include <type_traits>
 
+#include "key_ranges.hpp"
 #include "pot_device.hpp"
 #include "pot_launch.hpp"
 #include "score_decoded.hpp"
@@ -76,7 +77,6 @@ constexpr int kWaves = kBlock / 64;  // waves per workgroup of the default varia
 // Every engine but the fp16 comparator has it.
 template <int MODE, int K, int VF>
 constexpr int kPoolWaves = pool_waves(MODE, K, VF);
-constexpr int kWTile = 64;    // keys per wave tile
 constexpr float kPScale = 12.0f;  // p is formed as 2^(x - M + 12) (fp16-normal range)
 // 4-bit values: weights are formed as 2^(x - R + 8) s and may grow to 2^16 (fp16's range) before
 // the reference R rises.
@@ -284,7 +284,7 @@ __device__ __forceinline__ void plane_bits(const KeyRegs<MODE, K>& r, int s, uin
 // whose weights it forms in stage 2.
 // Blocks kFirst .. kEnd - 1 of the two K-blocks; the exponents come with block 0.
 // 4-bit values: one 16-byte load per K-block holds the lane's fragments of all four
-// dimension blocks (the record's order in pot_device.hpp), and the steps and minima of the
+// dimension blocks (the record's order in key_ranges.hpp), and the steps and minima of the
 // 8 keys whose weights the lane forms stand behind the values of their group.
 template <int VK, int kFirst = 0, int kEnd = 2>
 __device__ __forceinline__ void load_values_buf(const Streams& st, int t0, int lane,
@@ -292,12 +292,12 @@ __device__ __forceinline__ void load_values_buf(const Streams& st, int t0, int l
   constexpr bool V8 = VK == kValI8;
   if constexpr (VK == kValI4) {
     const BufRsrc rv = tile_rsrc(st.values, t0, st.v_end, kI4GroupBytes / 8);
-    const int part = (lane & 15) >> 3, grp = lane >> 4;
-    const int voff = tile_offset(grp * kI4GroupBytes + (lane & 15) * 16, t0);
+    constexpr int kBlockBytes = value_offset_i4(0, 1);
+    const int voff = tile_offset(value_offset_i4(lane, 0), t0);
 #pragma unroll
-    for (int kb = kFirst; kb < kEnd; ++kb) v.f[kb] = load_b128(rv, voff + kb * 4 * kI4GroupBytes, true);
+    for (int kb = kFirst; kb < kEnd; ++kb) v.f[kb] = load_b128(rv, voff + kb * kBlockBytes, true);
     if constexpr (kFirst == 0) {
-      const int soff = tile_offset((4 * part + grp) * kI4GroupBytes + kI4Steps, t0);
+      const int soff = tile_offset(step_offset_i4(lane), t0);
       v.s = load_b128(rv, soff, false);
       v.z = load_b128(rv, soff + kI4Minima - kI4Steps, false);
     }
@@ -748,12 +748,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   if constexpr (V4) {
     if (a.seq_lens != nullptr) {
       t_all = min(max(a.seq_lens[b], 0), a.T);
-      split_len = ((t_all + a.n_splits - 1) / a.n_splits + kWTile - 1) / kWTile * kWTile;
+      split_len = own_split_len(t_all, a.n_splits);
     }
   }
-  const int t_begin = split * split_len;
-  const int t_end = min(t_all, t_begin + split_len);
-  const int n_tiles = (t_end - t_begin + kWTile - 1) / kWTile;
+  const KeyRange range = split_range(t_all, split, split_len);
+  const int t_begin = range.begin, t_end = range.end, n_tiles = range.tiles;
   const int row = lane & 15, grp = lane >> 4, hrow = row & 7, part = row >> 3;
   const bool hvalid = hrow < G;
 
@@ -766,7 +765,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
   // The sequence's new token (fused append) belongs to the workgroup whose
   // range holds row T - 1.
   const bool appends = (MODE == kScorePot || MODE == kScoreDs4a) && a.app_k != nullptr &&
-                       (V4 ? t_begin < t_all && t_end == t_all
+                       (V4 ? holds_last(range, t_all)
                            : split == a.n_splits - 1);  // uniform per workgroup
   int gref = 0;
   float lsum = 0.0f;  // INT8 and 4-bit values: this lane's sum of the unscaled weights
@@ -800,10 +799,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
 
   KeyRegs<MODE, K> kr[2];
   constexpr int kNext = V4 ? 0 : 1;  // where the next tile's keys go
-  const int g_last = (t_end - 1) & ~7;  // first token of the range's last 8-token group
   Streams st{};
   st.t_end = t_end;
-  st.v_end = g_last + 8;
+  st.v_end = groups_end(range);
   if constexpr (MODE == kScorePot || MODE == kScoreDs4a) {
     st.codes = a.codes_se + row0 * (kDim / 2);
     st.scales = reinterpret_cast<const uint8_t*>(a.key_scale + row0);

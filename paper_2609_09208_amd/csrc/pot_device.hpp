@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "key_ranges.hpp"
 #include "pot_launch.hpp"
 
 namespace potattn {
@@ -249,14 +250,7 @@ __device__ __forceinline__ int store_value_token_i8_wave(const uint16_t* __restr
   return g;
 }
 
-// 4-bit values: groups of 8 tokens, kI4GroupBytes bytes each. Byte 16 (d % 16) +
-// 8 (d / 32) + t % 8 of a group has the n of dimension d in its low half where
-// d % 32 < 16 and in its high half elsewhere, so 16 consecutive bytes are the
-// matrix-core operands of 8 tokens for the dimensions c, 16 + c, 32 + c and 48 + c,
-// and a token has its bytes to itself; behind them the tokens' 8 fp16 steps s and 8
-// fp16 minima z. A value is z + s n.
-constexpr int kI4Steps = 256, kI4Minima = 272, kI4GroupBytes = 288;
-
+// 4-bit values (layout of a group in key_ranges.hpp).
 // The row's step: the smallest fp16 number >= fl(fl(max - min) / 15), as bits.
 // lo and hi are fp16 numbers, so the range is at most 131008 and s at most 8736.
 // The quotient is the correctly rounded one: a product with the rounded reciprocal and
