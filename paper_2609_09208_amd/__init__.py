@@ -71,10 +71,11 @@ def make_rope(rot_dim: int = HEAD_DIM, neighbours: bool = False, axis_of_pair=No
               head_dim: int = HEAD_DIM) -> pot_rope:
     """Rotation of a head's first rot_dim elements; axis_of_pair: the position axis of
     each of its rot_dim/2 pairs (None: one axis)."""
+    if rot_dim % 2 or not 0 <= rot_dim <= HEAD_DIM:
+        _mismatch("rot_dim: even, 0 to 64")
     axes = [0] * (rot_dim // 2) if axis_of_pair is None else [int(a) for a in axis_of_pair]
     if len(axes) != rot_dim // 2 or not all(0 <= a < POT_MAX_AXES for a in axes):
-        raise PotError(POT_ERR_INVALID_ARG, "POT_ERR_INVALID_ARG",
-                       "axis_of_pair: one axis, 0 to 3, for each of the rot_dim / 2 pairs")
+        _mismatch("axis_of_pair: one axis, 0 to 3, for each of the rot_dim / 2 pairs")
     return pot_rope(head_dim, rot_dim, int(bool(neighbours)), max(axes, default=0) + 1,
                     (ctypes.c_uint8 * 32)(*axes))
 
@@ -408,7 +409,10 @@ def _part(x, weight, out, tokens, dtype, device, out_type):
     """(B, S) and heads of a projection's rows [B, S, heads, 64] (any strides, elements side by
     side; of `tokens`, if given), and their pot_part. The output is dense [B, heads, S, 64] (of
     out_type, if given)."""
-    b, s, h, d = x.shape
+    try:
+        b, s, h, d = x.shape
+    except ValueError:  # not four dimensions
+        _mismatch("rows [B, S, heads, 64] are needed")
     sb, ss, sh, se = x.stride()
     at = b, s
     if (d != HEAD_DIM or se != 1 or x.dtype is not dtype or x.get_device() != device

@@ -95,3 +95,18 @@ def test_tensors_of_another_device(monkeypatch, current):
         pa.pot_norm_rope(pa.make_rope(0), rows, None, None, None, None, 0.0, None, None, OnGpu(torch.zeros((1, 4, 1, 64))), None,
                          None)
     assert "current device" in str(e.value)
+
+
+@pytest.mark.parametrize("rot_dim", [66, 128, -2, 3, 65])
+def test_a_rope_wider_than_a_head(rot_dim):
+    with pytest.raises(pa.PotError) as e:
+        pa.make_rope(rot_dim)
+    assert e.value.status == pa.POT_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("shape", [(6, 64), (2, 3, 64), (1, 2, 3, 4, 64)])
+def test_rows_of_other_dimensions(shape):
+    rows = OnGpu(torch.zeros(shape))
+    with pytest.raises(pa.PotError) as e:
+        pa.pot_norm_rope(pa.make_rope(), rows, None, None, None, None, 0.0, None, None, rows, None, None)
+    assert e.value.status == pa.POT_ERR_INVALID_ARG
