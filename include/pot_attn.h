@@ -284,8 +284,8 @@ typedef struct pot_part {
  *    y = x / sqrt(mean x^2 + eps) * w             (where there are weights w)
  *    (a, b) -> (a cos f - b sin f, b cos f + a sin f), f = position * inv_freq[i],
  * for pair i with the position on its axis. Values v pass as they are. All in fp32
- * (the angle in fp64, so that far positions keep their place in the turn), one
- * rounding at the end.
+ * (the angle in fp64, so that far positions keep their place in the turn; the mean of
+ * squares for rows of any finite size), one rounding at the end.
  *  dtype        pot_dtype of the rows.
  *  parts        HOST array {q, k, v}: [B][S][Hq], [B][S][Hkv] and [B][S][Hkv] rows of 64
  *               elements, e.g. the parts of one packed projection. q's output is of
@@ -297,7 +297,8 @@ typedef struct pot_part {
  *  Hq, Hkv      up to 1024 each (POT_ERR_UNSUPPORTED above).
  *  positions    int64 [n_axes][B][S], device, any sign, 8-byte aligned (not read if
  *               rot_dim = 0). The angle is exact to 2^-52 of itself plus rounding: for
- *               |position * inv_freq| up to 2^31 within 1e-6.
+ *               |position * inv_freq| up to 2^31 within 1e-6. It has to stay below 2^50,
+ *               where an fp64 number still tells a quarter of a turn from the next.
  *  inv_freq     double [rot_dim/2], device: radians per position (not read if
  *               rot_dim = 0).
  * Outputs alias nothing. B or S of 0 is a no-op; B * S up to 2^28. */

@@ -6,7 +6,9 @@
 // A row is one head of one token: 64 elements over 8 lanes, 8 rows a wave. The bound is
 // the memory stream (every row read and written once); the sum of squares takes three
 // DPP steps, and where the halves of a head are paired over its full width a lane works
-// on four elements of either half, so that pairs meet in registers.
+// on four elements of either half, so that pairs meet in registers. Halves of a part of the
+// head meet through LDS and make every angle twice: 32768 tokens of bf16 66.2 us with 32 and
+// 67.0 with 48 elements turned, against 65.8 with all 64.
 // Angles: position * inv_freq / 2 pi in fp64, whose whole turns are taken off exactly,
 // then sine and cosine by their series on an eighth of a turn in fp32.
 #include <type_traits>
