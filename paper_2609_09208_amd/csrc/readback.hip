@@ -96,7 +96,7 @@ struct KeysIn {
 // Eight rows a wave: lane l has elements 8 (l % 8) ..+7 of row l / 8. Where all its scales
 // are fp16 numbers (row maxima of fp16 keys are) one packed multiplication rounds the
 // product as the fp32 one and its conversion do. 2.1 M rows, k = 0 to 4: 47, 62, 68, 68 and
-// 71 us, 5.6 to 7.2 TB/s (a plane's bytes are one a lane, of 64 contiguous ones a plane).
+// 71 us, 5.6 to 7.2 TB/s (plane bytes by one a lane, eight of a row side by side).
 template <int K>
 __global__ __launch_bounds__(kBlock) void load_keys_kernel(const KeysIn in, RowRange r,
                                                            uint16_t* __restrict__ out) {
