@@ -1054,7 +1054,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
 
   // 4-bit values: the tile's weights (in hw, lw) and their sums. In the hot loop the
   // exponents are one multiply-add, and true is returned if a weight is out of range: the
-  // reference has to rise, nothing is summed yet. RAISED: raise4 has put the exponents in
+  // reference has to rise, nothing is summed yet. After raise4 (raised) the exponents are in
   // xv, and weights are at most 2^8.
   float psum = 0.0f, pzsum = 0.0f;
   auto weights4 = [&](auto raised, bool tail, int k0) -> bool {
@@ -1326,7 +1326,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(
     if (lane_m < 8) sm.wl[wave][lane_m] = lsum;
   } else {
     // rows 4 grp_m + r, the same in every column: column r hands over row r
-    const float sum = row_m == 0 ? acc[4][0] : row_m == 1 ? acc[4][1] : row_m == 2 ? acc[4][2] : acc[4][3];
+    const float sum = row_m == 0   ? acc[4][0]
+                      : row_m == 1 ? acc[4][1]
+                      : row_m == 2 ? acc[4][2]
+                                   : acc[4][3];
     const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum),
                                                     false, false);
     if (lane_m < 32 && row_m < 4)

@@ -104,3 +104,25 @@ def test_weights_of_a_part_left_out_are_not_looked_at(part):
         if other is None:
             out.copy_(got)
         assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("tokens", [11, 1033])
+@pytest.mark.parametrize("normed", ["q", "k"])
+@pytest.mark.parametrize("rot_dim,neighbours", [(64, False), (64, True), (32, False), (0, False)])
+def test_one_part_normed_and_the_other_not(tokens, normed, rot_dim, neighbours):
+    """Eight heads of a token share a wave where there are few tokens: five of q and three of k here."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    x = torch.randn((1, tokens, 11, 64), generator=g, device=DEV).to(torch.bfloat16)
+    q, k, v = x[:, :, :5], x[:, :, 5:8], x[:, :, 8:]
+    w = 1 + 0.2 * torch.randn(64, generator=g, device=DEV)
+    weights = (w, None) if normed == "q" else (None, w)
+    pos = torch.randint(0, 5000, (1, 1, tokens), generator=g, device=DEV)
+    outs = (torch.empty((1, 5, tokens, 64), device=DEV), *(torch.empty((1, 3, tokens, 64), dtype=torch.float16, device=DEV)
+                                                         for _ in range(2)))
+    pa.pot_norm_rope(pa.make_rope(rot_dim, neighbours), q, k, v, *weights, 1e-6, pos, _inv_freq(rot_dim), *outs)
+    for rows, weight, out, ty, turn in ((q, weights[0], outs[0], "fp32", True), (k, weights[1], outs[1], "fp16", True),
+                                        (v, None, outs[2], "fp16", False)):
+        want, size = _reference(rows, weight, 1e-6, pos, _inv_freq(rot_dim), [0] * (rot_dim // 2), rot_dim, neighbours, turn)
+        bound = (want.abs() * HALF_UNIT[ty] + SMALLEST[ty]) * (1 + 2.0 ** -8) + size * (16 * 2.0 ** -24 + 5000 * 2.0 ** -51)
+        assert ((out.cpu().double() - want).abs() <= bound).all()
