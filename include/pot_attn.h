@@ -307,6 +307,105 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* pa
                          const double* inv_freq, int32_t B, int32_t S, int32_t Hq, int32_t Hkv,
                          int32_t q_out_dtype, void* stream);
 
+/* How the values of a paged cache are held. */
+typedef enum pot_values { POT_VALUES_FP16 = 0, POT_VALUES_INT4 = 1 } pot_values;
+
+/* A paged cache: a pool of pages of page_size tokens for all kv heads, and the pages that each
+ * sequence has. Token t of sequence b, kv head h, is row (p * Hkv + h) * page_size + t % page_size
+ * of the pool with p = table[b][t / page_size]. The pool's arrays are those of a contiguous cache
+ * with (page, head) in the place of a sequence and page_size in that of t_cap, so pot_encode_keys,
+ * the value stores and the read-back calls work on pages too (n_seq = n_pages * Hkv), and a
+ * contiguous cache is a paged one whose only page per sequence is b.
+ *  codes_se, codes_m, key_scale : key codes (16-, 8- and 16-byte aligned; codes_m NULL iff k = 0).
+ *  values       : as pot_store_values writes them (POT_VALUES_FP16), or pot_store_values_int4
+ *                 (POT_VALUES_INT4); 16-byte aligned.
+ *  table        : device int32 [B][table_len]: page numbers. An entry outside [0, n_pages) is no
+ *                 page: its keys are not seen and its tokens are stored nowhere. Entries of pages
+ *                 that no query of a call sees are not followed where whole 64-key tiles lie
+ *                 between them and what is seen.
+ *  value_format : pot_values.
+ *  page_size    : a multiple of 8, up to 2^24.
+ *  Hkv          : 1 .. 128. n_pages * Hkv * page_size up to 2^40. */
+typedef struct pot_pages {
+  uint8_t* codes_se;
+  uint8_t* codes_m;
+  float* key_scale;
+  void* values;
+  const int32_t* table;
+  int32_t value_format;
+  int32_t n_pages;
+  int32_t Hkv;
+  int32_t page_size;
+  int32_t table_len;
+} pot_pages;
+
+/* New tokens of any number of sequences into a paged cache: pot_norm_rope of a projection's rows,
+ * then pot_encode_keys (row absmax scales) and the value store on the pages where the tokens
+ * belong, in one call; codes, scales, values and queries are those of the three calls bit for bit.
+ * The rows of the sequences stand side by side: rows cu_new[b] .. cu_new[b + 1] - 1 are the newest
+ * tokens of sequence b, the last ones of its seq_lens[b] (counted with them).
+ *  fmt          the cache's key format.
+ *  rope, dtype, weight_dtype, eps, inv_freq, q_out_dtype : as pot_norm_rope.
+ *  parts        HOST array {q, k, v}: [n][Hq], [n][Hkv] and [n][Hkv] rows of 64 elements
+ *               (stride_s: from token to token; stride_b is not read). q.out is dense
+ *               [n][Hq][64]; q may be left out. k and v are needed, their out is NULL.
+ *  positions    int64 [n_axes][n], device, or NULL: a token's place in its sequence, on every
+ *               axis.
+ *  cu_new       device int32 [B + 1], ascending; seq_lens device int32 [B], up to 2^24. Rows
+ *               outside cu_new[0] .. cu_new[B] - 1 are left as they are, in the queries too, so a
+ *               captured call may have more rows than a replay brings tokens. A token whose place
+ *               is negative is stored nowhere.
+ *  n            rows, up to 2^23. B up to 65535.
+ * Two tokens that come to the same cache row leave one of them or a mixture. Outputs alias
+ * nothing. B or n of 0 is a no-op. */
+pot_status pot_paged_append(const pot_format* fmt, const pot_rope* rope, int32_t dtype,
+                            const pot_part* parts, int32_t weight_dtype, float eps,
+                            const int64_t* positions, const double* inv_freq,
+                            const pot_pages* pages, const int32_t* cu_new,
+                            const int32_t* seq_lens, int32_t B, int32_t n, int32_t Hq,
+                            int32_t q_out_dtype, void* stream);
+
+/* Workspace bytes of pot_paged_attention for these sizes (any window). Host-only; 0 for invalid
+ * ones. */
+size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, int32_t max_new,
+                                 int32_t max_len);
+
+/* Causal attention of sequences' new tokens over their pages: chunks of prompts, single tokens, or
+ * both in one call. The new tokens are in the cache already (pot_paged_append). The query at place
+ * t of its sequence sees the keys at places j <= t, with a window only those with j > t - window
+ * or j < n_sink (the first tokens, which stay visible):
+ *    O = sum_j p_j v_j / sum_j p_j,  p_j = exp(q^ . K^_j / 8)
+ * with q^ and K^ as pot_decode_attention has them (INT8 query, rotated if fmt->hadamard; exact
+ * sums, here by codes decoded to fp16 weights on the matrix cores) and v_j the fp16 numbers that
+ * the cache stands for: as stored, or z + s n rounded once to fp16. Sums are fp32; weights enter
+ * the value products as fp16 numbers rounded to nearest, for outputs of 32 bits with what the
+ * rounding left added. A query that sees no key gets O = 0. What is not seen (later tokens, tokens
+ * outside the window, rows past a sequence's end, infinities and NaN there) never reaches O; an
+ * infinite or NaN value that is seen makes its element of O infinite or NaN (which is not defined).
+ * Scores, in the log2 domain, may lie anywhere in fp32's range.
+ *  dtype, out_dtype  pot_dtype of q and of out.
+ *  q            element m of query head h of row i is q[i * stride_t + h * stride_h + m], device,
+ *               16-byte aligned like every row.
+ *  cu_new, seq_lens  as pot_paged_append, with the same meaning. Rows of no sequence are left as
+ *               they are in out.
+ *  kv_head_of_q HOST int32 [Hq], every kv head serving the same number of query heads (any);
+ *               Hq up to 128.
+ *  max_new, max_len  the most new tokens and the longest length that a sequence may have: the
+ *               launch is planned for them. Further new tokens are not computed, keys past max_len
+ *               not seen. max_len up to 2^24 - 8 and up to table_len * page_size.
+ *  window       0: none. n_sink: not read without a window.
+ *  out          dense [n][Hq][64], device, 16-byte aligned; may not alias q or the cache.
+ *  workspace    >= pot_paged_workspace_bytes(...) bytes, 256-byte aligned; any contents. Calls that
+ *               share one must not overlap in time.
+ * Results do not differ from call to call. B or n of 0 is a no-op. n up to 2^23, B up to 65535. */
+pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void* q,
+                               int64_t stride_t, int64_t stride_h, const pot_pages* pages,
+                               const int32_t* cu_new, const int32_t* seq_lens,
+                               const int32_t* kv_head_of_q, int32_t B, int32_t n, int32_t Hq,
+                               int32_t max_new, int32_t max_len, int32_t window, int32_t n_sink,
+                               int32_t out_dtype, void* out, void* workspace, size_t ws_bytes,
+                               void* stream);
+
 /* Workspace bytes pot_decode_attention needs for this problem shape: the
  * key-split partials (M_s, l_s, o_s) for the largest split count the planner
  * can choose, and room of each (batch, kv head, split) at its head, of which

@@ -62,7 +62,16 @@ class pot_part(ctypes.Structure):
                 ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p)]
 
 
+class pot_pages(ctypes.Structure):
+    _fields_ = [("codes_se", ctypes.c_void_p), ("codes_m", ctypes.c_void_p),
+                ("key_scale", ctypes.c_void_p), ("values", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("value_format", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("table_len", ctypes.c_int32)]
+
+
 POT_FP16, POT_BF16, POT_FP32 = 0, 1, 2
+POT_VALUES_FP16, POT_VALUES_INT4 = 0, 1
 POT_INT4_GROUP_BYTES = 288
 POT_MAX_AXES = 4
 
@@ -135,6 +144,11 @@ def _load_library():
         "pot_load_values_int4": (i32, [P, i64, i64, i64, i64, P, P]),
         "pot_norm_rope": (i32, [ctypes.POINTER(pot_rope), i32, P, i32, ctypes.c_float, P, P, i32,
                                 i32, i32, i32, i32, P]),
+        "pot_paged_append": (i32, [fmt_p, ctypes.POINTER(pot_rope), i32, P, i32, ctypes.c_float, P, P,
+                                   ctypes.POINTER(pot_pages), P, P, i32, i32, i32, i32, P]),
+        "pot_paged_workspace_bytes": (S, [i32, i32, i32, i32, i32, i32]),
+        "pot_paged_attention": (i32, [fmt_p, i32, P, i64, i64, ctypes.POINTER(pot_pages), P, P, P, i32,
+                                      i32, i32, i32, i32, i32, i32, i32, P, P, S, P]),
         "pot_int8_encode_keys": (i32, [P, i64, i64, i32, P, P, P]),
         "pot_int8_decode_attention": (i32, [P, P, P, P, i64, P, i32, i32, i32,
                                             i32, i32, P, P, S, dbg_p, P]),
@@ -486,6 +500,146 @@ def pot_norm_rope(rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, posit
         _check(status)
 
 
+def make_pages(codes_se, codes_m, key_scale, values, table) -> pot_pages:
+    """A pool of pages and the pages of each sequence, from tensors as alloc_pages makes them: codes_se
+    [n_pages, Hkv, page_size, 32], codes_m [.., 8k] or None, key_scale [n_pages, Hkv, page_size], values
+    float16 [n_pages, Hkv, page_size, 64] or uint8 [n_pages, Hkv, page_size / 8, 288], table int32 [B, entries],
+    dense, on one GPU. The tensors are kept by the result, and their contents may change between calls."""
+    if codes_se.dim() != 4 or table.dim() != 2:
+        _mismatch("codes_se [n_pages, Hkv, page_size, 32] and a table [B, entries] are needed")
+    n_pages, Hkv, page_size = codes_se.shape[:3]
+    int4 = values.dtype is torch.uint8
+    want = [(codes_se, torch.uint8, (n_pages, Hkv, page_size, HEAD_DIM // 2)),
+            (key_scale, torch.float32, (n_pages, Hkv, page_size)), (table, torch.int32, tuple(table.shape)),
+            (values, torch.uint8, (n_pages, Hkv, page_size // 8, POT_INT4_GROUP_BYTES)) if int4 else
+            (values, torch.float16, (n_pages, Hkv, page_size, HEAD_DIM))]
+    if codes_m is not None:
+        k = codes_m.shape[-1] // 8
+        if not 1 <= k <= 4:
+            _mismatch("codes_m is [n_pages, Hkv, page_size, 8k], k = 1 to 4")
+        want.append((codes_m, torch.uint8, (n_pages, Hkv, page_size, 8 * k)))
+    device = table.get_device()
+    for t, dtype, shape in want:
+        if (t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.get_device() != device):
+            _mismatch("dense tensors of one pool on one GPU are needed")
+    pages = pot_pages(_ptr(codes_se), _ptr(codes_m), _ptr(key_scale), _ptr(values), _ptr(table),
+                      POT_VALUES_INT4 if int4 else POT_VALUES_FP16, n_pages, Hkv, page_size, table.shape[1])
+    pages.tensors = (codes_se, codes_m, key_scale, values, table)
+    return pages
+
+
+def _sequences(pages, cu_new, seq_lens, device) -> int:
+    """B of a call over pages, whose sequences' bounds and lengths the kernels read as int32."""
+    table = pages.tensors[4]
+    B = table.shape[0]
+    if (cu_new.dtype is not torch.int32 or seq_lens.dtype is not torch.int32 or cu_new.numel() != B + 1
+            or seq_lens.numel() != B or not cu_new.is_contiguous() or not seq_lens.is_contiguous()
+            or cu_new.get_device() != device or seq_lens.get_device() != device
+            or table.get_device() != device):
+        _mismatch("cu_new is dense int32 [B + 1], seq_lens [B], on the rows' GPU, as are the pages")
+    return B
+
+
+def _key_format(fmt, pages) -> None:
+    codes_m = pages.tensors[1]
+    if fmt.mant_bits != (0 if codes_m is None else codes_m.shape[-1] // 8):
+        _mismatch("the pages hold keys of another mant_bits")
+
+
+def _packed(x, heads, weight, out, dtype, device, n):
+    """pot_part of packed rows [n, heads, 64] (any strides, elements side by side)."""
+    if (x.dim() != 3 or x.shape[0] != n or x.shape[2] != HEAD_DIM or x.stride(2) != 1 or x.dtype is not dtype
+            or x.get_device() != device or (heads is not None and x.shape[1] != heads)):
+        _mismatch("rows [n, heads, 64] of one type with dense elements on one GPU are needed")
+    if weight is not None and (weight.numel() != HEAD_DIM or not weight.is_contiguous()
+                               or weight.get_device() != device):
+        _mismatch("weights are [64] and dense, on the rows' GPU")
+    if out is not None and (tuple(out.shape) != tuple(x.shape) or not out.is_contiguous()
+                            or out.get_device() != device):
+        _mismatch("a dense output [n, heads, 64] on the rows' GPU is needed")
+    return _pack_part(x.data_ptr(), 0, x.stride(0), x.stride(1), 0 if weight is None else weight.data_ptr(),
+                      0 if out is None else out.data_ptr())
+
+
+def pot_paged_append(fmt: pot_format, rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions,
+                     inv_freq, pages: pot_pages, cu_new, seq_lens, q_out, stream=None) -> None:
+    """q [n, Hq, 64] (or None), k and v [n, Hkv, 64] (tensors of one type, any strides): the newest tokens of
+    all sequences side by side, sequence b's being rows cu_new[b] .. cu_new[b + 1] - 1 and the last of its
+    seq_lens[b]; k and v go into the pages, q to q_out [n, Hq, 64] (dense). positions int64 [n_axes, n] or
+    None (places in the sequence), inv_freq float64 [rot_dim / 2], weights [64] of one type or None."""
+    dtype, device, n = k.dtype, k.get_device(), k.shape[0]
+    if device < 0:
+        _mismatch("tensors on the GPU are needed")
+    B = _sequences(pages, cu_new, seq_lens, device)
+    _key_format(fmt, pages)
+    Hq, parts = 0, _NO_PART
+    if q is not None:
+        if q_out is None:
+            _mismatch("q needs an output")
+        Hq, parts = q.shape[1], _packed(q, None, q_weight, q_out, dtype, device, n)
+    parts += _packed(k, pages.Hkv, k_weight, None, dtype, device, n)
+    parts += _packed(v, pages.Hkv, None, None, dtype, device, n)
+    if q is None:
+        q_weight = None
+    w = q_weight if q_weight is not None else k_weight
+    if k_weight is not None and k_weight.dtype is not w.dtype:
+        _mismatch("weights are of one type")
+    if positions is not None and (positions.dtype is not torch.int64 or not positions.is_contiguous()
+                                  or positions.numel() != rope.n_axes * n or positions.get_device() != device):
+        _mismatch("positions are dense int64 [n_axes, n] on the rows' GPU")
+    if inv_freq is not None and (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
+                                 or inv_freq.numel() < rope.rot_dim // 2 or inv_freq.get_device() != device):
+        _mismatch("inv_freq is dense float64 [rot_dim / 2] on the rows' GPU")
+    itype, wtype = _DTYPES.get(dtype), _DTYPES.get(dtype if w is None else w.dtype)
+    qtype = POT_FP32 if q is None else _DTYPES.get(q_out.dtype)
+    if itype is None or wtype is None or qtype is None:
+        _mismatch("types are float16, bfloat16 or float32")
+    status = _lib.pot_paged_append(
+        fmt, rope, itype, parts, wtype, eps, None if positions is None else positions.data_ptr(),
+        None if inv_freq is None else inv_freq.data_ptr(), pages, cu_new.data_ptr(), seq_lens.data_ptr(), B, n,
+        Hq, qtype, _stream(stream, device))
+    if status:
+        _check(status)
+
+
+def pot_paged_workspace_bytes(B: int, n: int, Hq: int, Hkv: int, max_new: int, max_len: int) -> int:
+    return int(_lib.pot_paged_workspace_bytes(B, n, Hq, Hkv, max_new, max_len))
+
+
+def pot_paged_attention(fmt: pot_format, q, pages: pot_pages, cu_new, seq_lens, kv_head_of_q, max_new: int,
+                        max_len: int, out, workspace, ws_bytes=None, window: int = 0, n_sink: int = 0,
+                        stream=None) -> None:
+    """q [n, Hq, 64] (any strides), the newest tokens of all sequences side by side (as pot_paged_append, whose
+    keys and values are in the pages), to out [n, Hq, 64] (dense). A query sees its sequence up to itself, with
+    a window the last `window` tokens of that and the first n_sink."""
+    try:
+        n, Hq, d = q.shape
+        st, sh, se = q.stride()
+    except ValueError:
+        _mismatch("queries [n, Hq, 64] are needed")
+    device = q.get_device()
+    if device < 0:
+        _mismatch("tensors on the GPU are needed")
+    if (d != HEAD_DIM or se != 1 or tuple(out.shape) != (n, Hq, d) or not out.is_contiguous()
+            or out.get_device() != device):
+        _mismatch("queries and a dense output [n, Hq, 64] on one GPU are needed")
+    B = _sequences(pages, cu_new, seq_lens, device)
+    _key_format(fmt, pages)
+    itype, otype = _DTYPES.get(q.dtype), _DTYPES.get(out.dtype)
+    if itype is None or otype is None:
+        _mismatch("types are float16, bfloat16 or float32")
+    heads, hp = _heads(kv_head_of_q)
+    if heads.size != Hq:
+        _mismatch("kv_head_of_q has Hq entries")
+    if workspace is not None and ws_bytes is None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    status = _lib.pot_paged_attention(
+        fmt, itype, q.data_ptr(), st, sh, pages, cu_new.data_ptr(), seq_lens.data_ptr(), hp, B, n, Hq, max_new,
+        max_len, window, n_sink, otype, out.data_ptr(), _ptr(workspace), ws_bytes or 0, _stream(stream, device))
+    if status:
+        _check(status)
+
+
 def pot_ds4a_decode_attention(fmt: pot_format, q, codes_se, key_scale, v_fp16, t_cap: int,
                               kv_head_of_q, B: int, Hq: int, Hkv: int, T: int, out,
                               workspace, ws_bytes=None, dbg: pot_debug | None = None,
@@ -569,6 +723,13 @@ def alloc_value_cache_int4(B: int, Hkv: int, t_cap: int, device):
     """4-bit value cache: uint8 [B,Hkv,t_cap/8,288], records of 8 tokens."""
     return torch.zeros((B, Hkv, t_cap // 8, POT_INT4_GROUP_BYTES), dtype=torch.uint8,
                        device=device)
+
+
+def alloc_pages(n_pages: int, Hkv: int, page_size: int, mant_bits: int, device, int4: bool = False):
+    """A pool of zeroed pages: (codes_se, codes_m or None, key_scale, values), as make_pages takes them."""
+    keys = alloc_pot_cache(n_pages, Hkv, page_size, mant_bits, device)
+    make = alloc_value_cache_int4 if int4 else alloc_value_cache
+    return keys["codes_se"], keys["codes_m"], keys["key_scale"], make(n_pages, Hkv, page_size, device)
 
 
 def alloc_workspace(nbytes: int, device):

@@ -520,6 +520,142 @@ pot_status check_part(const char* name, const pot_part& p, int32_t heads, int32_
   return POT_OK;
 }
 
+// What pot_norm_rope and pot_paged_append check and pass on alike.
+pot_status check_rope(const pot_rope& rope, int32_t dtype, int32_t weight_dtype, int32_t q_out_dtype,
+                      float eps) {
+  if (rope.head_dim != 64)
+    return fail(POT_ERR_UNSUPPORTED, "head_dim %d (only 64)", rope.head_dim);
+  const int r = rope.rot_dim;
+  if (r < 0 || r > 64 || r % 2)
+    return fail(POT_ERR_INVALID_ARG, "rot_dim %d (even, 0 .. 64)", r);
+  if (rope.neighbours != 0 && rope.neighbours != 1)
+    return fail(POT_ERR_INVALID_ARG, "neighbours %d (0 or 1)", rope.neighbours);
+  if (rope.n_axes < 1 || rope.n_axes > POT_MAX_AXES)
+    return fail(POT_ERR_INVALID_ARG, "n_axes %d (1 .. %d)", rope.n_axes, POT_MAX_AXES);
+  for (int i = 0; i < r / 2; ++i)
+    if (rope.axis_of_pair[i] >= rope.n_axes)
+      return fail(POT_ERR_INVALID_ARG, "axis_of_pair[%d] = %d outside [0, %d)", i,
+                  rope.axis_of_pair[i], rope.n_axes);
+  for (const int32_t t : {dtype, weight_dtype, q_out_dtype})
+    if (t < POT_FP16 || t > POT_FP32)
+      return fail(POT_ERR_INVALID_ARG, "type %d (0 fp16, 1 bf16, 2 fp32)", t);
+  if (!(eps >= 0.0f && eps <= 3.4e38f)) return fail(POT_ERR_INVALID_ARG, "eps %g", eps);
+  return POT_OK;
+}
+void fill_rope(const pot_rope& rope, int32_t dtype, int32_t weight_dtype, int32_t q_out_dtype, float eps,
+               NormRopeArgs* a) {
+  a->eps = eps;
+  a->dtype = dtype;
+  a->weight_dtype = weight_dtype;
+  a->q_out_dtype = q_out_dtype;
+  a->rot_dim = rope.rot_dim;
+  a->neighbours = rope.neighbours;
+  a->n_axes = rope.n_axes;
+  for (int i = 0; i < 32; ++i) a->axis_of_pair[i] = i < rope.rot_dim / 2 ? rope.axis_of_pair[i] : 0;
+}
+
+// A paged cache and the sequences of a call.
+pot_status check_pages(const pot_format* fmt, const pot_pages* p, const int32_t* cu_new,
+                       const int32_t* seq_lens, int32_t B, int32_t n, PagesArg* arg, PackedRows* rows) {
+  if (!p) return fail(POT_ERR_INVALID_ARG, "pages is NULL");
+  if (p->value_format != POT_VALUES_FP16 && p->value_format != POT_VALUES_INT4)
+    return fail(POT_ERR_INVALID_ARG, "value_format %d (0 fp16, 1 4-bit)", p->value_format);
+  if (p->Hkv < 1) return fail(POT_ERR_INVALID_ARG, "%d kv heads", p->Hkv);
+  if (p->Hkv > kMaxHqArg) return fail(POT_ERR_UNSUPPORTED, "Hkv %d > %d", p->Hkv, kMaxHqArg);
+  if (p->page_size < 8 || p->page_size % 8 || p->page_size > (1 << 24))
+    return fail(POT_ERR_INVALID_ARG, "page_size %d is not a multiple of 8 up to 2^24", p->page_size);
+  if (p->n_pages < 1 || p->table_len < 1)
+    return fail(POT_ERR_INVALID_ARG, "n_pages %d or table_len %d < 1", p->n_pages, p->table_len);
+  if ((int64_t)p->n_pages * p->Hkv > ((int64_t)1 << 40) / p->page_size)
+    return fail(POT_ERR_INVALID_ARG, "n_pages * Hkv * page_size too large");
+  if (B < 0 || n < 0) return fail(POT_ERR_INVALID_ARG, "B %d or n %d < 0", B, n);
+  if (B > 65535) return fail(POT_ERR_UNSUPPORTED, "B %d > 65535", B);
+  if (n > (1 << 23)) return fail(POT_ERR_UNSUPPORTED, "n %d > 2^23", n);
+  if ((fmt->mant_bits > 0) != (p->codes_m != nullptr))
+    return fail(POT_ERR_INVALID_ARG, "codes_m must be non-NULL exactly when mant_bits > 0");
+  if (!p->codes_se || !p->key_scale || !p->values || !p->table)
+    return fail(POT_ERR_INVALID_ARG, "codes_se, key_scale, values or table is NULL");
+  if (!aligned(p->codes_se, 16) || !aligned(p->codes_m, 8) || !aligned(p->key_scale, 16) ||
+      !aligned(p->values, 16) || !aligned(p->table, 4))
+    return fail(POT_ERR_INVALID_ARG, "misaligned codes_se / codes_m / key_scale / values / table");
+  if (!cu_new || !seq_lens) return fail(POT_ERR_INVALID_ARG, "cu_new or seq_lens is NULL");
+  if (!aligned(cu_new, 4) || !aligned(seq_lens, 4))
+    return fail(POT_ERR_INVALID_ARG, "cu_new and seq_lens must be 4-byte aligned");
+  const uint32_t groups = (uint32_t)p->page_size / 8;
+  *arg = PagesArg{p->codes_se, p->codes_m, p->key_scale, static_cast<uint8_t*>(p->values), p->table,
+                  p->n_pages, p->Hkv, p->table_len, (int32_t)groups, page_div(groups)};
+  *rows = PackedRows{cu_new, seq_lens, B, n};
+  return POT_OK;
+}
+
+pot_status check_paged_sizes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, int32_t max_new,
+                             int32_t max_len) {
+  if (B < 0 || n < 0 || Hq < 1 || Hkv < 1 || max_new < 1 || max_len < 1)
+    return fail(POT_ERR_INVALID_ARG, "bad sizes B=%d n=%d Hq=%d Hkv=%d max_new=%d max_len=%d", B, n, Hq, Hkv,
+                max_new, max_len);
+  if (B > 65535 || n > (1 << 23)) return fail(POT_ERR_UNSUPPORTED, "B %d > 65535 or n %d > 2^23", B, n);
+  if (Hq > kMaxHqArg) return fail(POT_ERR_UNSUPPORTED, "Hq %d > %d", Hq, kMaxHqArg);
+  if (Hq % Hkv) return fail(POT_ERR_UNSUPPORTED, "Hq %d not a multiple of Hkv %d", Hq, Hkv);
+  if (max_len > kMaxKeys) return fail(POT_ERR_UNSUPPORTED, "max_len %d > %d", max_len, kMaxKeys);
+  return POT_OK;
+}
+
+// Head map with groups of any one size, [Hkv][G] a byte each.
+pot_status check_head_groups(const int32_t* map, int Hq, int Hkv, uint32_t* q_of_kv) {
+  if (!map) return fail(POT_ERR_INVALID_ARG, "kv_head_of_q is NULL");
+  const int G = Hq / Hkv;
+  int fill[kMaxHqArg] = {};
+  for (int i = 0; i < Hq; ++i) {
+    const int h = map[i];
+    if (h < 0 || h >= Hkv)
+      return fail(POT_ERR_INVALID_ARG, "kv_head_of_q[%d] = %d outside [0, %d)", i, h, Hkv);
+    if (fill[h] >= G)
+      return fail(POT_ERR_UNSUPPORTED, "kv head %d serves more than %d query heads", h, G);
+    const int at = h * G + fill[h]++;
+    q_of_kv[at >> 2] |= (uint32_t)i << (8 * (at & 3));
+  }
+  return POT_OK;
+}
+
+// How a paged attention call is split. A longer max_len never takes fewer splits than a shorter one or
+// a window, so that the workspace of the former serves the latter.
+PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, int window, int n_sink) {
+  const int64_t G = Hq / Hkv, rows = std::min(max_new, n) * G;
+  int64_t keys = max_len;  // that a row tile sees, at most
+  if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + max_new + n_sink + 2 * kWTile);
+  const int64_t tiles = (keys + kWTile - 1) / kWTile;
+  PagedPlan p{};
+  const bool few = rows <= kFewRows, many = !few;
+  // one sequence, or all of them as long as they may be: nothing is left for the kernel of few rows
+  const bool both = many && G <= kFewRows && B > 1 && n < (int64_t)B * max_new;
+  if (few || both) {
+    p.few_limit = kFewRows;
+    const int64_t units = (int64_t)B * Hkv, most = (tiles + 3) / 4;
+    p.few_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({1024 / units, most, 64}));
+  }
+  if (many) {
+    p.many_waves = rows > 128 ? 8 : 4;
+    const int64_t R = 32 * p.many_waves, full = ((int64_t)n * G + R - 1) / R;
+    p.many_tiles = (int64_t)n * G / R + std::min(B, n);
+    const int64_t most = (tiles + 7) / 8;
+    p.many_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 * 8 / p.many_waves / (full * Hkv), most, 32}));
+  }
+  return p;
+}
+
+struct PagedLayout {
+  size_t many, total;
+};
+PagedLayout paged_layout(const PagedPlan& p, int B, int Hkv) {
+  PagedLayout w{};
+  if (p.few_splits > 1)
+    w.many = align_up((size_t)B * Hkv * p.few_splits * kFewRows * kPartial * 4, 256);
+  w.total = w.many;
+  if (p.many_splits > 1)
+    w.total += align_up((size_t)p.many_tiles * Hkv * p.many_splits * 32 * p.many_waves * kPartial * 4, 256);
+  return w;
+}
+
 }  // namespace
 
 extern "C" {
@@ -667,23 +803,9 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* pa
                          const double* inv_freq, int32_t B, int32_t S, int32_t Hq, int32_t Hkv,
                          int32_t q_out_dtype, void* stream) {
   if (!rope || !parts) return fail(POT_ERR_INVALID_ARG, "rope or parts is NULL");
-  if (rope->head_dim != 64)
-    return fail(POT_ERR_UNSUPPORTED, "head_dim %d (only 64)", rope->head_dim);
+  pot_status st = check_rope(*rope, dtype, weight_dtype, q_out_dtype, eps);
+  if (st != POT_OK) return st;
   const int r = rope->rot_dim;
-  if (r < 0 || r > 64 || r % 2)
-    return fail(POT_ERR_INVALID_ARG, "rot_dim %d (even, 0 .. 64)", r);
-  if (rope->neighbours != 0 && rope->neighbours != 1)
-    return fail(POT_ERR_INVALID_ARG, "neighbours %d (0 or 1)", rope->neighbours);
-  if (rope->n_axes < 1 || rope->n_axes > POT_MAX_AXES)
-    return fail(POT_ERR_INVALID_ARG, "n_axes %d (1 .. %d)", rope->n_axes, POT_MAX_AXES);
-  for (int i = 0; i < r / 2; ++i)
-    if (rope->axis_of_pair[i] >= rope->n_axes)
-      return fail(POT_ERR_INVALID_ARG, "axis_of_pair[%d] = %d outside [0, %d)", i,
-                  rope->axis_of_pair[i], rope->n_axes);
-  for (const int32_t t : {dtype, weight_dtype, q_out_dtype})
-    if (t < POT_FP16 || t > POT_FP32)
-      return fail(POT_ERR_INVALID_ARG, "type %d (0 fp16, 1 bf16, 2 fp32)", t);
-  if (!(eps >= 0.0f && eps <= 3.4e38f)) return fail(POT_ERR_INVALID_ARG, "eps %g", eps);
   if (B < 0 || S < 0 || Hq < 0 || Hkv < 0)
     return fail(POT_ERR_INVALID_ARG, "bad shape B=%d S=%d Hq=%d Hkv=%d", B, S, Hq, Hkv);
   if (Hq > 1024 || Hkv > 1024)
@@ -691,7 +813,7 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* pa
   if (B == 0 || S == 0) return ok();
   NormRopeArgs a{};
   const int size = dtype == POT_FP32 ? 4 : 2;
-  pot_status st = check_part("q", parts[0], Hq, B, S, size, &a.q);
+  st = check_part("q", parts[0], Hq, B, S, size, &a.q);
   if (st == POT_OK) st = check_part("k", parts[1], Hkv, B, S, size, &a.k);
   if (st == POT_OK) st = check_part("v", parts[2], Hkv, B, S, size, &a.v);
   if (st != POT_OK) return st;
@@ -710,19 +832,134 @@ pot_status pot_norm_rope(const pot_rope* rope, int32_t dtype, const pot_part* pa
   a.q_out = parts[0].out;
   a.k_out = static_cast<uint16_t*>(parts[1].out);
   a.v_out = static_cast<uint16_t*>(parts[2].out);
-  a.eps = eps;
   a.B = B;
   a.S = S;
   a.Hq = a.q.data ? Hq : 0;
   a.Hkv = a.k.data || a.v.data ? Hkv : 0;
-  a.dtype = dtype;
-  a.weight_dtype = weight_dtype;
-  a.q_out_dtype = q_out_dtype;
-  a.rot_dim = r;
-  a.neighbours = rope->neighbours;
-  a.n_axes = rope->n_axes;
-  for (int i = 0; i < 32; ++i) a.axis_of_pair[i] = i < r / 2 ? rope->axis_of_pair[i] : 0;
+  fill_rope(*rope, dtype, weight_dtype, q_out_dtype, eps, &a);
   return hip_status(launch_norm_rope(a, static_cast<hipStream_t>(stream)), "norm and rotation launch");
+}
+
+pot_status pot_paged_append(const pot_format* fmt, const pot_rope* rope, int32_t dtype,
+                            const pot_part* parts, int32_t weight_dtype, float eps,
+                            const int64_t* positions, const double* inv_freq,
+                            const pot_pages* pages, const int32_t* cu_new,
+                            const int32_t* seq_lens, int32_t B, int32_t n, int32_t Hq,
+                            int32_t q_out_dtype, void* stream) {
+  pot_status st = check_format(fmt);
+  if (st != POT_OK) return st;
+  if (!rope || !parts) return fail(POT_ERR_INVALID_ARG, "rope or parts is NULL");
+  st = check_rope(*rope, dtype, weight_dtype, q_out_dtype, eps);
+  if (st != POT_OK) return st;
+  PagedAppendArgs a{};
+  st = check_pages(fmt, pages, cu_new, seq_lens, B, n, &a.pages, &a.packed);
+  if (st != POT_OK) return st;
+  if (Hq < 0 || Hq > 1024) return fail(POT_ERR_UNSUPPORTED, "%d query heads (0 .. 1024)", Hq);
+  if (B == 0 || n == 0) return ok();
+  const int size = dtype == POT_FP32 ? 4 : 2, per16 = 16 / size;
+  NormRopeArgs& r = a.rows;
+  for (int i = 0; i < 3; ++i) {
+    static const char* const kName[3] = {"q", "k", "v"};
+    const pot_part& p = parts[i];
+    const int heads = i == 0 ? Hq : pages->Hkv;
+    if (i == 0 && !p.rows) {
+      if (p.out) return fail(POT_ERR_INVALID_ARG, "q is left out, but not its output");
+      continue;
+    }
+    if (!p.rows) return fail(POT_ERR_INVALID_ARG, "%s is NULL", kName[i]);
+    if (heads < 1) return fail(POT_ERR_INVALID_ARG, "%d heads of q", heads);
+    if ((i == 0) != (p.out != nullptr))
+      return fail(POT_ERR_INVALID_ARG, i == 0 ? "q has no output" : "%s goes into the pages: its out is NULL",
+                  kName[i]);
+    if (!aligned(p.rows, 16) || !aligned(p.out, 16) || !aligned(p.weight, 16) ||
+        (n > 1 && p.stride_s % per16) || (heads > 1 && p.stride_h % per16))
+      return fail(POT_ERR_INVALID_ARG, "rows, weight and output of %s must be 16-byte aligned", kName[i]);
+    (i == 0 ? r.q : i == 1 ? r.k : r.v) =
+        RowsIn{p.rows, 0, n > 1 ? p.stride_s : 0, heads > 1 ? p.stride_h : 0};
+  }
+  if (parts[2].weight) return fail(POT_ERR_INVALID_ARG, "v takes no weight");
+  if (rope->rot_dim > 0 && !inv_freq) return fail(POT_ERR_INVALID_ARG, "inv_freq is NULL");
+  if (!aligned(positions, 8) || !aligned(inv_freq, 8))
+    return fail(POT_ERR_INVALID_ARG, "positions and inv_freq must be 8-byte aligned");
+  r.q_weight = r.q.data ? parts[0].weight : nullptr;
+  r.k_weight = parts[1].weight;
+  r.positions = positions;
+  r.inv_freq = inv_freq;
+  r.q_out = parts[0].out;
+  r.B = 1;
+  r.S = n;
+  r.Hq = r.q.data ? Hq : 0;
+  r.Hkv = pages->Hkv;
+  fill_rope(*rope, dtype, weight_dtype, q_out_dtype, eps, &r);
+  a.tab = encode_tables(fmt->mant_bits);
+  a.hadamard = fmt->hadamard;
+  a.value_format = pages->value_format;
+  return hip_status(launch_paged_append(a, static_cast<hipStream_t>(stream)), "paged append launch");
+}
+
+size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, int32_t max_new,
+                                 int32_t max_len) {
+  if (check_paged_sizes(B, n, Hq, Hkv, max_new, max_len) != POT_OK) return 0;
+  if (B == 0 || n == 0) return 0;
+  return paged_layout(paged_plan(B, n, Hq, Hkv, max_new, max_len, 0, 0), B, Hkv).total;
+}
+
+pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void* q,
+                               int64_t stride_t, int64_t stride_h, const pot_pages* pages,
+                               const int32_t* cu_new, const int32_t* seq_lens,
+                               const int32_t* kv_head_of_q, int32_t B, int32_t n, int32_t Hq,
+                               int32_t max_new, int32_t max_len, int32_t window, int32_t n_sink,
+                               int32_t out_dtype, void* out, void* workspace, size_t ws_bytes,
+                               void* stream) {
+  pot_status st = check_format(fmt);
+  if (st != POT_OK) return st;
+  for (const int32_t t : {dtype, out_dtype})
+    if (t < POT_FP16 || t > POT_FP32)
+      return fail(POT_ERR_INVALID_ARG, "type %d (0 fp16, 1 bf16, 2 fp32)", t);
+  PagedAttendArgs a{};
+  st = check_pages(fmt, pages, cu_new, seq_lens, B, n, &a.pages, &a.packed);
+  if (st == POT_OK) st = check_paged_sizes(B, n, Hq, pages->Hkv, max_new, max_len);
+  if (st != POT_OK) return st;
+  if (max_len > (int64_t)pages->table_len * pages->page_size)
+    return fail(POT_ERR_INVALID_ARG, "max_len %d > %d pages of %d", max_len, pages->table_len, pages->page_size);
+  if (window < 0 || n_sink < 0)
+    return fail(POT_ERR_INVALID_ARG, "window %d or n_sink %d < 0", window, n_sink);
+  st = check_head_groups(kv_head_of_q, Hq, pages->Hkv, a.q_of_kv);
+  if (st != POT_OK) return st;
+  if (B == 0 || n == 0) return ok();
+  if (!q || !out) return fail(POT_ERR_INVALID_ARG, "q or out is NULL");
+  const int per16 = dtype == POT_FP32 ? 4 : 8;
+  if (!aligned(q, 16) || !aligned(out, 16) || (n > 1 && stride_t % per16) || (Hq > 1 && stride_h % per16))
+    return fail(POT_ERR_INVALID_ARG, "q's rows and out must be 16-byte aligned");
+  // past the longest sequence a window takes nothing off
+  a.window = window >= (1 << 24) ? 0 : window;
+  a.n_sink = std::min(n_sink, 1 << 24);
+  a.plan = paged_plan(B, n, Hq, pages->Hkv, max_new, max_len, a.window, a.n_sink);
+  const PagedLayout w = paged_layout(a.plan, B, pages->Hkv);
+  if (w.total > 0 && !workspace) return fail(POT_ERR_INVALID_ARG, "workspace is NULL");
+  if (!aligned(workspace, 256))
+    return fail(POT_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (ws_bytes < w.total)
+    return fail(POT_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, w.total);
+  a.q = q;
+  a.q_stride_t = n > 1 ? stride_t : 0;
+  a.q_stride_h = Hq > 1 ? stride_h : 0;
+  a.out = out;
+  a.few_part = static_cast<float*>(workspace);
+  a.many_part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.many);
+  a.Hq = Hq;
+  a.G = Hq / pages->Hkv;
+  a.max_new = max_new;
+  a.max_len = max_len;
+  a.dtype = dtype;
+  a.out_dtype = out_dtype;
+  a.hadamard = fmt->hadamard;
+  a.mant_bits = fmt->mant_bits;
+  a.value_format = pages->value_format;
+  hipError_t e = hipSuccess;
+  if (a.plan.many_splits > 0) e = launch_paged_many(a, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess && a.plan.few_splits > 0) e = launch_paged_few(a, static_cast<hipStream_t>(stream));
+  return hip_status(e, "paged attention launch");
 }
 
 size_t pot_decode_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t T) {

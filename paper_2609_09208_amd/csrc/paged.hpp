@@ -1,0 +1,212 @@
+// What the kernels of the paged cache share: where a sequence's tokens stand, its new rows,
+// queries as score operands, and the values' fp16 numbers.
+#pragma once
+
+#include "encode_rows.hpp"
+#include "head_rows.hpp"
+#include "page_ranges.hpp"
+#include "pot_device.hpp"
+#include "pot_launch.hpp"
+
+namespace potattn {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// First cache row / 8 of group `group` of a sequence for a kv head: group `in` of its page;
+// -1 where the table has no such page. table: the sequence's entries.
+__device__ __forceinline__ int64_t group_row8(const PagesArg& p, const int32_t* table, int kvh,
+                                              int group) {
+  const uint32_t page = page_of_group((uint32_t)group, p.div);
+  if (group < 0 || page >= (uint32_t)p.table_len) return -1;
+  const int32_t at = table[page];
+  if ((uint32_t)at >= (uint32_t)p.n_pages) return -1;
+  return ((int64_t)at * p.Hkv + kvh) * p.page_groups + (group - (int)page * p.page_groups);
+}
+
+__device__ __forceinline__ NewTokens sequence_tokens(const PackedRows& r, int b, int most_new,
+                                                     int most_len) {
+  return new_tokens(r.cu_new[b], r.cu_new[b + 1], r.seq_lens[b], r.n, most_new, most_len);
+}
+
+// 8 natural elements of a row (16-byte aligned) as floats. Every lane of a row takes part.
+__device__ __forceinline__ void load8(const void* base, int64_t at, int chunk, int type,
+                                      float (&x)[8]) {
+  if (type == POT_FP32) to_floats<POT_FP32, kNeighbours>(load_row<POT_FP32, kNeighbours>(base, at, chunk), x);
+  else if (type == POT_BF16) to_floats<POT_BF16, kNeighbours>(load_row<POT_BF16, kNeighbours>(base, at, chunk), x);
+  else to_floats<POT_FP16, kNeighbours>(load_row<POT_FP16, kNeighbours>(base, at, chunk), x);
+}
+
+// Walsh-Hadamard rotation of a row over its 8 lanes (lane g: elements 8g .. 8g + 7), fp64
+// stages of span 1 .. 32, one rounding to fp32.
+__device__ __forceinline__ void rotate_hadamard(float (&x)[8], int lane) {
+  double v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (double)x[i];
+#pragma unroll
+  for (int h = 1; h < 8; h <<= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((i & h) == 0) {
+        const double p = v[i], q = v[i + h];
+        v[i] = p + q;
+        v[i + h] = p - q;
+      }
+  const double s1 = butterfly_sign<1>(lane), s2 = butterfly_sign<2>(lane), s4 = butterfly_sign<4>(lane);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = butterfly<1>(v[i], s1);
+    v[i] = butterfly<2>(v[i], s2);
+    v[i] = butterfly<4>(v[i], s4);
+    x[i] = (float)(v[i] * 0.125);
+  }
+}
+
+// The INT8 query of a row over its 8 lanes as fp16 integers, in the order of decode_weights
+// (elements 0 4 1 5 2 6 3 7 of the lane's 8), and its score factor: with the weights' 2^-8
+// taken back, sum * scale * factor is the score times log2 e.
+__device__ __forceinline__ uint4 quantised_query(float (&x)[8], int hadamard, int lane, float* factor) {
+  if (hadamard) rotate_hadamard(x, lane);
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+  top = max_over_8_lanes(top);
+  int q[8];
+  const float inv = 127.0f / top;  // correctly rounded divisions
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = top == 0.0f ? 0 : quantize_int8(x[i], inv);
+  *factor = __fmul_rn(top / 127.0f, log2e_f32()) * 32.0f;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_half((float)q[i], (float)q[i + 4]);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Code dword w (nibble n: element n) and its mantissa planes' bytes (bit n: element n) as the
+// fp16 weights sigma (1 + j / 2^K) 2^(-8 - e), in the order 0 4 1 5 2 6 3 7: sign bit, exponent
+// field 7 - e, the mantissa bits on top of fp16's; the zero code (e = 7) is exponent field 0,
+// where the mantissa bits are taken off whatever they are.
+template <int K>
+__device__ __forceinline__ half8 paged_weights(uint32_t w, const uint32_t* planes) {
+  const uint32_t nx = ~w;
+  uint32_t zero = 0;  // bit 4n + 3: element n is the zero code
+  uint32_t pl[K > 0 ? K : 1];
+  if constexpr (K > 0) {
+    zero = (w & 0x77777777u) + 0x11111111u;
+#pragma unroll
+    for (int b = 0; b < K; ++b) pl[b] = (planes[b] & 0xFu) | ((planes[b] << 12) & 0xF0000u);
+  }
+  uint32_t v[4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    v[n] = (n < 3 ? nx << (n < 3 ? 10 - 4 * n : 0) : nx >> 2) & 0x1C001C00u;
+    if constexpr (K > 0) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int b = 0; b < K; ++b) m |= ((pl[b] >> n) & 0x00010001u) << (10 - K + b);
+      const uint32_t z = (zero >> (4 * n + 3)) & 0x00010001u;
+      v[n] |= m & ~((z << 10) - z);
+    }
+    v[n] |= (w << (12 - 4 * n)) & 0x80008000u;
+  }
+  return __builtin_bit_cast(half8, make_uint4(v[0], v[1], v[2], v[3]));
+}
+
+// fp16 values z + s n of 8 tokens, each rounded once (a packed multiply-add), from the tokens'
+// n (bytes of w0, w1, below 16) and their steps and minima, two a dword.
+__device__ __forceinline__ uint4 int4_values(uint32_t w0, uint32_t w1, const uint4& s, const uint4& z) {
+  constexpr uint32_t kExp = 0x64646464u;  // a byte under it: 1024 + n
+  const uint32_t n4[4] = {__builtin_amdgcn_perm(kExp, w0, 0x04010400u),
+                          __builtin_amdgcn_perm(kExp, w0, 0x04030402u),
+                          __builtin_amdgcn_perm(kExp, w1, 0x04010400u),
+                          __builtin_amdgcn_perm(kExp, w1, 0x04030402u)};
+  const uint32_t s4[4] = {s.x, s.y, s.z, s.w}, z4[4] = {z.x, z.y, z.z, z.w};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const half2v c = {(_Float16)-1024.0f, (_Float16)-1024.0f};
+    const half2v n = __builtin_bit_cast(half2v, n4[i]) + c;
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(n, __builtin_bit_cast(half2v, s4[i]),
+                                                                  __builtin_bit_cast(half2v, z4[i])));
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// Tokens at or past `end` of the 8 from `first` on to 0: whatever the cache holds there cannot
+// reach the sums.
+__device__ __forceinline__ uint4 mask_tokens(uint4 v, int first, int end) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] &= ((first + 2 * i < end) ? 0x0000FFFFu : 0u) | ((first + 2 * i + 1 < end) ? 0xFFFF0000u : 0u);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Values that are infinite or NaN, in tiles of which some query sees a part only: their product
+// with a weight of 0 would be NaN where they are not seen. They go into the sums as 0, and
+// beside those the matrix cores count them for the keys that a query sees.
+__device__ __forceinline__ bool has_special(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    any |= (w[i] & 0x7C00u) == 0x7C00u || (w[i] & 0x7C000000u) == 0x7C000000u;
+  return any;
+}
+__device__ __forceinline__ void split_special(const half8& v, half8* rest, half8* marks) {
+  const uint4 u = __builtin_bit_cast(uint4, v);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w}, kOne = 0x3C003C00u;
+  uint32_t r[4], m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t off = ((w[i] & 0x7C00u) == 0x7C00u ? 0x0000FFFFu : 0u) |
+                         ((w[i] & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
+    r[i] = w[i] & ~off;
+    m[i] = kOne & off;
+  }
+  *rest = __builtin_bit_cast(half8, make_uint4(r[0], r[1], r[2], r[3]));
+  *marks = __builtin_bit_cast(half8, make_uint4(m[0], m[1], m[2], m[3]));
+}
+// What the counted values make of a sum.
+__device__ __forceinline__ float special_sum(float count) {
+  return count > 0.0f ? __builtin_nanf("") : 0.0f;
+}
+
+// Weights of fp32 as fp16 operands: rounded to nearest, and what that left, rounded in turn.
+__device__ __forceinline__ uint32_t low_part(float a, float b, uint32_t hi) {
+  const half2v h = __builtin_bit_cast(half2v, hi);
+  return pack_half(a - (float)h.x, b - (float)h.y);
+}
+
+// A row's output from its weighted sums, 4 neighbouring elements, in the output's type.
+__device__ __forceinline__ void store_out4(void* out, int64_t at, int type, float a, float b, float c,
+                                           float d) {
+  if (type == POT_FP32)
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(a, b, c, d);
+  else if (type == POT_BF16)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+  else
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack_half(a, b), pack_half(c, d));
+}
+__device__ __forceinline__ void store_out1(void* out, int64_t at, int type, float a) {
+  if (type == POT_FP32) static_cast<float*>(out)[at] = a;
+  else if (type == POT_BF16) static_cast<uint16_t*>(out)[at] = (uint16_t)pack_bf16(a, a);
+  else static_cast<uint16_t*>(out)[at] = (uint16_t)pack_half(a, a);
+}
+
+// A key's weight: y its sum times its scale, m the query's reference, c its factor. Weights are
+// formed as 2^(x - m + 7) and the reference rises once a key is more than 2^8 over it, so the
+// largest of a query's lies between 2^7 and 2^15 and fp16's normal numbers reach 2^-21 of it at
+// the least.
+constexpr float kWeightShift = 7.0f, kMostRise = 8.0f;
+__device__ __forceinline__ float paged_weight(float y, float m, float c) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(y - m, c, kWeightShift));
+}
+
+// 2^((m - M) c) of two references (-inf: nothing summed yet), c >= 0.
+__device__ __forceinline__ float between(float m, float M, float c) {
+  return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - M) * c);
+}
+
+}  // namespace potattn

@@ -1,0 +1,336 @@
+// Attention over a paged cache for sequences with many rows (new tokens x query heads of a kv
+// head): chunks of prompts. A workgroup takes a tile of 32 NW rows of one sequence and kv head,
+// 32 rows a wave, and goes through the 64-key tiles that some of its rows see; the keys' codes
+// and the values become fp16 operands in LDS once for all its waves, the next tile's loads under
+// way meanwhile.
+//
+// Scores S^T = K Q^T by v_mfma_f32_32x32x16_f16 (codes as fp16 weights, the INT8 queries as fp16
+// integers: exact sums), the rows of K in such an order that a lane ends up with the scores of
+// one query and 8 consecutive keys of every 16: the operand of O^T = V^T P^T as they stand. A
+// query's reference, sum and outputs are its two lanes' own. The reference rises only when a weight would
+// leave fp16's range.
+#pragma once
+
+#include "paged.hpp"
+
+namespace potattn {
+
+// Row tiles of a sequence.
+__device__ __forceinline__ int many_tiles_of(const PagedAttendArgs& a, int b, int R) {
+  if (b >= a.packed.B) return 0;
+  const NewTokens t = sequence_tokens(a.packed, b, a.max_new, a.max_len);
+  const int rows = t.n * a.G;
+  return t.n <= a.plan.few_limit && rows <= a.plan.few_limit ? 0 : (rows + R - 1) / R;
+}
+// Tile i of all, counted from the last sequence's last: a prompt's late tiles, which see the
+// most keys, come first. b < 0: there is none. Every lane of the wave takes part.
+struct RowTile {
+  int b, tile;
+};
+__device__ __forceinline__ RowTile find_tile(const PagedAttendArgs& a, int i, int R) {
+  const int lane = lane_id();
+  int total = 0;
+  for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
+    int n = many_tiles_of(a, b0 + lane, R);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
+    total += n;
+  }
+  i = __builtin_amdgcn_readfirstlane(total) - 1 - i;
+  if (i < 0) return {-1, 0};
+  for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
+    const int n = many_tiles_of(a, b0 + lane, R);
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(sum, o, 64);
+      sum += lane >= o ? v : 0;
+    }
+    const uint64_t past = __ballot(sum > i);
+    if (past != 0) {
+      const int at = (int)__builtin_ctzll(past);
+      return {b0 + at, i - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(n, at))};
+    }
+    i -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return {-1, 0};
+}
+
+template <int VF>
+struct ManyStage {  // what a lane loads of a group of 8 keys
+  uint32_t code, plane[4];
+  float scale;
+  uint4 v;
+};
+template <>
+struct ManyStage<POT_VALUES_INT4> {
+  uint32_t code, plane[4];
+  float scale;
+  uint2 n;
+  uint4 s, z;
+};
+
+// LOW: the weights' rounding goes into the products too (outputs of 32 bits).
+template <int K, int VF, int NW, bool LOW>
+__global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendArgs a) {
+  constexpr int R = 32 * NW, kGroups = 8 / NW;  // groups a wave stages
+  struct Tile {
+    uint4 k[8 * 64];  // chunk d (dimensions 8d ..+7) of key j at 64 d + (j ^ d)
+    uint4 v[8 * 64];  // tokens 8g ..+7 of dimension d at 64 g + d
+  };
+  __shared__ Tile tiles[2];
+  __shared__ __attribute__((aligned(16))) float scales[2][64];
+  __shared__ __attribute__((aligned(16))) int flags[2][8];  // of a group: 1 not there, 2 holds special values
+  static_assert(sizeof(tiles) >= sizeof(uint4) * R * 8, "the queries pass through the tiles' place");
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int S = a.plan.many_splits, Hkv = a.pages.Hkv;
+  const int split = blockIdx.x % S, kvh = blockIdx.x / S % Hkv, index = blockIdx.x / S / Hkv;
+  const RowTile at = find_tile(a, index, R);
+  if (at.b < 0) return;
+  const NewTokens t = sequence_tokens(a.packed, at.b, a.max_new, a.max_len);
+  const int rows = t.n * a.G, r0 = at.tile * R;
+  const int last = min(r0 + R, rows) - 1;
+  const SeenTiles seen = seen_tiles(t.place + r0 / a.G, t.place + last / a.G, t.len, a.window, a.n_sink);
+  const TileRun run = split_tiles(seen.tiles, split, S);
+  const int wg_first = t.place + r0 / a.G, wg_last = t.place + last / a.G;
+  const int32_t* table = a.pages.table + (int64_t)at.b * a.pages.table_len;
+
+  // ---- queries: 8 rows of the wave at a time, 8 lanes each ---------------------------------
+  const int col = lane & 31, half = lane >> 5;
+  uint4* sq = reinterpret_cast<uint4*>(tiles) + wave * 32 * 8;
+  float c = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int rw = 8 * i + (lane >> 3), r = r0 + 32 * wave + rw;
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (r < rows) {
+      const int tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));
+      load8(a.q, (int64_t)(t.first + tok) * a.q_stride_t + head * a.q_stride_h, lane & 7, a.dtype, x);
+    }
+    float factor;
+    sq[rw * 8 + (lane & 7)] = quantised_query(x, a.hadamard, lane, &factor);
+    // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants row col's
+    const float got = __shfl(factor, 8 * (col & 7), 64);
+    if ((col >> 3) == i) c = got;
+  }
+  __syncthreads();
+  half8 q[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) q[s] = __builtin_bit_cast(half8, sq[col * 8 + 2 * s + half]);
+  __syncthreads();
+
+  const int my_row = r0 + 32 * wave + col;
+  const bool active = r0 + 32 * wave < rows;
+  const int place = t.place + min(my_row, last) / a.G;
+  const int w_first = t.place + min(r0 + 32 * wave, last) / a.G;
+  const int w_last = t.place + min(r0 + 32 * wave + 31, last) / a.G;
+
+  // ---- staging: wave w has groups w, w + NW .. of the tile --------------------------------
+  ManyStage<VF> st[kGroups];
+  bool st_there[kGroups];
+  auto load = [&](int j) {
+    const int g0 = tile_start(seen, j) / 8;
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const int g = g0 + wave + NW * i;
+      const int64_t row8 = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
+      st_there[i] = row8 >= 0;
+      st[i] = ManyStage<VF>{};
+      if (row8 >= 0) {
+        const int64_t row = row8 * 8 + (lane >> 3);
+        st[i].code = *reinterpret_cast<const uint32_t*>(a.pages.codes_se + row * 32 + 4 * (lane & 7));
+#pragma unroll
+        for (int p = 0; p < K; ++p) st[i].plane[p] = a.pages.codes_m[row * 8 * K + 8 * p + (lane & 7)];
+        if (lane < 8) st[i].scale = a.pages.key_scale[row8 * 8 + lane];
+        if constexpr (VF == POT_VALUES_INT4) {
+          const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
+          st[i].n = *reinterpret_cast<const uint2*>(rec + 16 * (lane & 15) + 8 * (lane >> 5));
+          st[i].s = *reinterpret_cast<const uint4*>(rec + kI4Steps);
+          st[i].z = *reinterpret_cast<const uint4*>(rec + kI4Minima);
+        } else {
+          st[i].v = *reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim) + 16 * lane);
+        }
+      }
+    }
+  };
+  auto stage = [&](int j, int buf) {
+    const int t0 = tile_start(seen, j);
+    const bool part = !all_seen(wg_first, wg_last, t0, a.window, a.n_sink);
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const int g = wave + NW * i, key = 8 * g + (lane >> 3), d = lane & 7;
+      tiles[buf].k[64 * d + (key ^ d)] = __builtin_bit_cast(uint4, paged_weights<K>(st[i].code, st[i].plane));
+      uint4 v;
+      if constexpr (VF == POT_VALUES_INT4) {
+        const int sh = (lane & 16) ? 4 : 0;
+        v = int4_values((st[i].n.x >> sh) & 0x0F0F0F0Fu, (st[i].n.y >> sh) & 0x0F0F0F0Fu, st[i].s, st[i].z);
+      } else {
+        v = st[i].v;
+      }
+      int flag = st_there[i] ? 0 : 1;
+      if (part) {  // uniform
+        v = mask_tokens(v, t0 + 8 * g, seen.end);
+        if (__any(has_special(v))) flag |= 2;
+      }
+      tiles[buf].v[64 * g + lane] = v;
+      if (lane < 8) scales[buf][8 * g + lane] = st[i].scale;
+      if (lane == 0) flags[buf][g] = flag;
+    }
+  };
+
+  f32x16 acc[2];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[0][i] = acc[1][i] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+  // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
+  const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
+
+  auto compute = [&](int t0, int buf) {
+    if (!active || none_seen(w_first, w_last, t0, a.window, a.n_sink)) return;
+    const Tile& T = tiles[buf];
+    const int4 f0 = *reinterpret_cast<const int4*>(&flags[buf][0]);
+    const int4 f1 = *reinterpret_cast<const int4*>(&flags[buf][4]);
+    const int any = __builtin_amdgcn_readfirstlane(f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w);
+    const bool part = !all_seen(w_first, w_last, t0, a.window, a.n_sink) || (any & 1);
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
+#pragma unroll
+      for (int step = 0; step < 4; ++step) {
+        const int d = 2 * step + half;
+        const half8 kv = __builtin_bit_cast(half8, T.k[64 * d + ((32 * kb + krow) ^ d)]);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q[step], s[kb], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float4* sp = reinterpret_cast<const float4*>(&scales[buf][32 * kb + 16 * u + 8 * half]);
+        const float4 a0 = sp[0], a1 = sp[1];
+        const float sv[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[kb][8 * u + i] *= sv[i];
+      }
+    if (part) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bool there = !(flags[buf][4 * kb + 2 * u + half] & 1);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int key = t0 + 32 * kb + 16 * u + 8 * half + i;
+            if (!(there && key < seen.end && sees(place, key, a.window, a.n_sink))) s[kb][8 * u + i] = -INFINITY;
+          }
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+    const bool rises = top > m && (m == -INFINITY || (top - m) * c > kMostRise);
+    if (__any(rises)) {
+      const float to = rises ? top : m, f = between(m, to, c);
+      acc[0] *= f;
+      acc[1] *= f;
+      l *= f;
+      m = to;
+    }
+    uint32_t hi[16], lo[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int kb = i >> 3, e = 2 * (i & 7);
+      float p0 = paged_weight(s[kb][e], m, c), p1 = paged_weight(s[kb][e + 1], m, c);
+      if (part) {
+        p0 = s[kb][e] == -INFINITY ? 0.0f : p0;
+        p1 = s[kb][e + 1] == -INFINITY ? 0.0f : p1;
+      }
+      l += p0;
+      l += p1;
+      hi[i] = pack_half(p0, p1);
+      if constexpr (LOW) lo[i] = low_part(p0, p1, hi[i]);
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {  // 16 keys at a time
+      const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[4 * b], hi[4 * b + 1], hi[4 * b + 2], hi[4 * b + 3]));
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) {
+        half8 v = __builtin_bit_cast(half8, T.v[64 * (2 * b + half) + 32 * nb + col]);
+        if (part && (any & 2)) {  // uniform
+          half8 marks, ones;
+          split_special(v, &v, &marks);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            ones[i] = s[b >> 1][8 * (b & 1) + i] == -INFINITY ? (_Float16)0.0f : (_Float16)1.0f;
+          f32x16 n;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+          n = __builtin_amdgcn_mfma_f32_32x32x16_f16(marks, ones, n, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[nb][i] += special_sum(n[i]);
+        }
+        acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[nb], 0, 0, 0);
+        if constexpr (LOW) {
+          const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[4 * b], lo[4 * b + 1], lo[4 * b + 2], lo[4 * b + 3]));
+          acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[nb], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  int buf = 0;
+  if (run.first < run.end) {
+    load(run.first);
+    stage(run.first, 0);
+  }
+  // a barrier a tile: it stands between the staging of a place and its use, and between its use
+  // and its next staging, which comes a tile later
+  for (int j = run.first; j < run.end; ++j) {
+    __syncthreads();
+    if (j + 1 < run.end) load(j + 1);
+    compute(tile_start(seen, j), buf);
+    if (j + 1 < run.end) stage(j + 1, buf ^ 1);
+    buf ^= 1;
+  }
+
+  const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
+  if (my_row >= rows) return;
+  if (S == 1) {
+    const int tok = my_row / a.G, head = a.q_head(kvh * a.G + (my_row - tok * a.G));
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t base = ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * half;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        store_out4(a.out, base + 32 * nb + 8 * i, a.out_dtype, acc[nb][4 * i] * inv, acc[nb][4 * i + 1] * inv,
+                   acc[nb][4 * i + 2] * inv, acc[nb][4 * i + 3] * inv);
+    return;
+  }
+  float* part = a.many_part + ((((int64_t)index * Hkv + kvh) * S + split) * R + (my_row - r0)) * kPartial;
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(part + 32 * nb + 8 * i + 4 * half) =
+          f32x4{acc[nb][4 * i], acc[nb][4 * i + 1], acc[nb][4 * i + 2], acc[nb][4 * i + 3]};
+  if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{m, l, c, 0.0f};
+}
+
+template <int K, int VF, int NW>
+hipError_t launch_many(const PagedAttendArgs& a, hipStream_t stream) {
+  const dim3 grid((uint32_t)(a.plan.many_tiles * a.pages.Hkv * a.plan.many_splits));
+  if (a.out_dtype == POT_FP32)
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, NW, true>), grid, dim3(64 * NW), 0, stream, a);
+  else
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, NW, false>), grid, dim3(64 * NW), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace potattn

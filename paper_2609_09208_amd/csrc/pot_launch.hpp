@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "page_ranges.hpp"
 #include "pot_attn.h"
 
 namespace potattn {
@@ -194,5 +195,65 @@ struct NormRopeArgs {
   uint8_t axis_of_pair[32];
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, hipStream_t stream);
+
+// A pool of pages and the pages of every sequence (pot_pages).
+struct PagesArg {
+  uint8_t* codes_se;
+  uint8_t* codes_m;
+  float* key_scale;
+  uint8_t* values;       // fp16 values or 4-bit records
+  const int32_t* table;  // [B][table_len]
+  int32_t n_pages, Hkv, table_len;
+  int32_t page_groups;   // groups of 8 tokens in a page
+  PageDiv div;           // by page_groups
+};
+
+// New tokens of sequences side by side.
+struct PackedRows {
+  const int32_t* cu_new;    // [B + 1]
+  const int32_t* seq_lens;  // [B]
+  int32_t B, n;             // sequences, rows
+};
+
+struct PagedAppendArgs {
+  NormRopeArgs rows;  // B = 1, S = the packed rows; k_out and v_out unused; positions may be NULL
+  PagesArg pages;
+  PackedRows packed;
+  EncodeTables tab;
+  int32_t hadamard, value_format;
+};
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
+
+// Rows (new token x query head of a kv head) that the kernel of few rows takes of a sequence.
+constexpr int kFewRows = 16;
+// How a call is split: the kernel of few rows in few_splits key ranges, the kernel of many in
+// tiles of 32 many_waves rows and many_splits ranges; splits of 0: not launched. Sequences of up
+// to few_limit rows go to the former.
+struct PagedPlan {
+  int32_t few_limit, few_splits, many_splits, many_waves;
+  int64_t many_tiles;  // an upper bound
+};
+// Floats of one row's partial: 64 sums, the reference, the weights' sum and the score factor.
+constexpr int kPartial = 68;
+
+struct PagedAttendArgs {
+  const void* q;
+  int64_t q_stride_t, q_stride_h;  // elements
+  void* out;
+  float* few_part;   // [B][Hkv][few_splits][kFewRows][kPartial]
+  float* many_part;  // [tiles][Hkv][many_splits][rows of a tile][kPartial]
+  PagesArg pages;
+  PackedRows packed;
+  PagedPlan plan;
+  int32_t Hq, G, max_new, max_len;
+  int32_t window, n_sink;
+  int32_t dtype, out_dtype;
+  int32_t hadamard, mant_bits, value_format;
+  uint32_t q_of_kv[kMaxHqArg / 4];  // as DecodeArgs::q_of_kv
+
+  __host__ __device__ int q_head(int i) const { return (q_of_kv[i >> 2] >> (8 * (i & 3))) & 0xFF; }
+};
+hipError_t launch_paged_few(const PagedAttendArgs& a, hipStream_t stream);
+hipError_t launch_paged_many(const PagedAttendArgs& a, hipStream_t stream);
 
 }  // namespace potattn

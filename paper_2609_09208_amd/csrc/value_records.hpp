@@ -6,16 +6,11 @@
 
 namespace potattn {
 
-// A record of 8 tokens by a wave. Lane l has dimensions 8g .. 8g + 7 (g = l % 8) of token
-// l / 8, 16 bytes; a group is one contiguous KiB. Its 8 lanes find the token's minimum and
-// maximum. The n of lanes g and g ^ 2 (dimensions 16 apart) share bytes: each of the two
-// makes four of the eight (one exchange), and two exchanges over the token's low bits then
-// give every lane a dword of four tokens, 4 bytes of the record's 256. t: the lane's token
-// in the range, first: that of its dword's first; n_tok for uint32 comparisons, full: all
-// eight are there (uniform).
-__device__ __forceinline__ void store_record(const uint4 v, uint8_t* __restrict__ out, int lane,
-                                             bool full, int t, int first, uint32_t n_tok) {
-  const int g = lane & 7, u = lane >> 3;
+// A token's n over its 8 lanes as the bytes that the record has them in: lane g gets columns
+// 8 (g % 2) + 4 (g / 2 % 2) + j (j = 0 .. 3, byte j) of half g / 4. Its step and minimum too.
+__device__ __forceinline__ uint32_t record_columns(const uint4 v, int lane, uint16_t* step_out,
+                                                   float* lo_out) {
+  const int g = lane & 7;
   const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
   float x[8];
 #pragma unroll
@@ -58,8 +53,24 @@ __device__ __forceinline__ void store_record(const uint4 v, uint8_t* __restrict_
   // bytes of dimension pairs (c, c + 16): lane bit 1 is that of the 16
   const bool upper = (g & 2) != 0;
   const uint32_t got = lane_xor_u32<2>(upper ? b[0] : b[1]);
-  uint32_t d = upper ? (got | (b[1] << 4)) : (b[0] | (got << 4));
-  d = transpose_tokens(d, lane);
+  *step_out = step;
+  *lo_out = lo;
+  return upper ? (got | (b[1] << 4)) : (b[0] | (got << 4));
+}
+
+// A record of 8 tokens by a wave. Lane l has dimensions 8g .. 8g + 7 (g = l % 8) of token
+// l / 8, 16 bytes; a group is one contiguous KiB. Its 8 lanes find the token's minimum and
+// maximum. The n of lanes g and g ^ 2 (dimensions 16 apart) share bytes: each of the two
+// makes four of the eight (one exchange), and two exchanges over the token's low bits then
+// give every lane a dword of four tokens, 4 bytes of the record's 256. t: the lane's token
+// in the range, first: that of its dword's first; n_tok for uint32 comparisons, full: all
+// eight are there (uniform).
+__device__ __forceinline__ void store_record(const uint4 v, uint8_t* __restrict__ out, int lane,
+                                             bool full, int t, int first, uint32_t n_tok) {
+  const int g = lane & 7, u = lane >> 3;
+  uint16_t step;
+  float lo;
+  const uint32_t d = transpose_tokens(record_columns(v, lane, &step, &lo), lane);
   const int at = record_offset(lane);
   if (full) {
     *reinterpret_cast<uint32_t*>(out + at) = d;
