@@ -325,7 +325,8 @@ typedef enum pot_values { POT_VALUES_FP16 = 0, POT_VALUES_INT4 = 1 } pot_values;
  *                 between them and what is seen.
  *  value_format : pot_values.
  *  page_size    : a multiple of 8, up to 2^24.
- *  Hkv          : 1 .. 128. n_pages * Hkv * page_size up to 2^40. */
+ *  Hkv          : 1 .. 128. n_pages * Hkv * page_size up to 2^33 (576 GiB of
+ *                 the smallest rows). */
 typedef struct pot_pages {
   uint8_t* codes_se;
   uint8_t* codes_m;

@@ -566,7 +566,7 @@ pot_status check_pages(const pot_format* fmt, const pot_pages* p, const int32_t*
     return fail(POT_ERR_INVALID_ARG, "page_size %d is not a multiple of 8 up to 2^24", p->page_size);
   if (p->n_pages < 1 || p->table_len < 1)
     return fail(POT_ERR_INVALID_ARG, "n_pages %d or table_len %d < 1", p->n_pages, p->table_len);
-  if ((int64_t)p->n_pages * p->Hkv > ((int64_t)1 << 40) / p->page_size)
+  if ((int64_t)p->n_pages * p->Hkv > ((int64_t)1 << 33) / p->page_size)
     return fail(POT_ERR_INVALID_ARG, "n_pages * Hkv * page_size too large");
   if (B < 0 || n < 0) return fail(POT_ERR_INVALID_ARG, "B %d or n %d < 0", B, n);
   if (B > 65535) return fail(POT_ERR_UNSUPPORTED, "B %d > 65535", B);
@@ -619,7 +619,8 @@ pot_status check_head_groups(const int32_t* map, int Hq, int Hkv, uint32_t* q_of
 
 // How a paged attention call is split. A longer max_len never takes fewer splits than a shorter one or
 // a window, so that the workspace of the former serves the latter.
-PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, int window, int n_sink) {
+PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, int window, int n_sink,
+                     int few_per_cu) {
   const int64_t G = Hq / Hkv, rows = std::min(max_new, n) * G;
   int64_t keys = max_len;  // that a row tile sees, at most
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + max_new + n_sink + 2 * kWTile);
@@ -631,7 +632,7 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
   if (few || both) {
     p.few_limit = kFewRows;
     const int64_t units = (int64_t)B * Hkv, most = (tiles + 3) / 4;
-    p.few_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({1024 / units, most, 64}));
+    p.few_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 * few_per_cu / units, most, 64}));
   }
   if (many) {
     p.many_waves = rows > 128 ? 8 : 4;
@@ -901,7 +902,7 @@ size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, 
                                  int32_t max_len) {
   if (check_paged_sizes(B, n, Hq, Hkv, max_new, max_len) != POT_OK) return 0;
   if (B == 0 || n == 0) return 0;
-  return paged_layout(paged_plan(B, n, Hq, Hkv, max_new, max_len, 0, 0), B, Hkv).total;
+  return paged_layout(paged_plan(B, n, Hq, Hkv, max_new, max_len, 0, 0, few_simd_waves(0, true)), B, Hkv).total;
 }
 
 pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void* q,
@@ -934,7 +935,8 @@ pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void*
   // past the longest sequence a window takes nothing off
   a.window = window >= (1 << 24) ? 0 : window;
   a.n_sink = std::min(n_sink, 1 << 24);
-  a.plan = paged_plan(B, n, Hq, pages->Hkv, max_new, max_len, a.window, a.n_sink);
+  a.plan = paged_plan(B, n, Hq, pages->Hkv, max_new, max_len, a.window, a.n_sink,
+                      few_simd_waves(fmt->mant_bits, pages->page_size % kWTile == 0));
   const PagedLayout w = paged_layout(a.plan, B, pages->Hkv);
   if (w.total > 0 && !workspace) return fail(POT_ERR_INVALID_ARG, "workspace is NULL");
   if (!aligned(workspace, 256))

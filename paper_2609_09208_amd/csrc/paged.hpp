@@ -14,15 +14,15 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+// A group's rows of the pool are counted by groups: row8 = row / 8, below 2^31.
 // First cache row / 8 of group `group` of a sequence for a kv head: group `in` of its page;
 // -1 where the table has no such page. table: the sequence's entries.
-__device__ __forceinline__ int64_t group_row8(const PagesArg& p, const int32_t* table, int kvh,
-                                              int group) {
+__device__ __forceinline__ int group_row8(const PagesArg& p, const int32_t* table, int kvh, int group) {
   const uint32_t page = page_of_group((uint32_t)group, p.div);
   if (group < 0 || page >= (uint32_t)p.table_len) return -1;
   const int32_t at = table[page];
   if ((uint32_t)at >= (uint32_t)p.n_pages) return -1;
-  return ((int64_t)at * p.Hkv + kvh) * p.page_groups + (group - (int)page * p.page_groups);
+  return (at * p.Hkv + kvh) * p.page_groups + (group - (int)page * p.page_groups);
 }
 
 __device__ __forceinline__ NewTokens sequence_tokens(const PackedRows& r, int b, int most_new,
@@ -86,29 +86,37 @@ __device__ __forceinline__ uint4 quantised_query(float (&x)[8], int hadamard, in
 // Code dword w (nibble n: element n) and its mantissa planes' bytes (bit n: element n) as the
 // fp16 weights sigma (1 + j / 2^K) 2^(-8 - e), in the order 0 4 1 5 2 6 3 7: sign bit, exponent
 // field 7 - e, the mantissa bits on top of fp16's; the zero code (e = 7) is exponent field 0,
-// where the mantissa bits are taken off whatever they are.
+// where the mantissa bits are taken off whatever they are. The numbers' high bytes are looked up,
+// four codes an operation: 12 operations for 8 codes at K = 0.
+__device__ __forceinline__ uint32_t spread_nibbles(uint32_t x) {  // bit n of 8 to bit 4n
+  x = (x | (x << 12)) & 0x000F000Fu;
+  x = (x | (x << 6)) & 0x03030303u;
+  return (x | (x << 3)) & 0x11111111u;
+}
 template <int K>
 __device__ __forceinline__ half8 paged_weights(uint32_t w, const uint32_t* planes) {
-  const uint32_t nx = ~w;
-  uint32_t zero = 0;  // bit 4n + 3: element n is the zero code
-  uint32_t pl[K > 0 ? K : 1];
+  constexpr uint32_t kLut0 = 0x1014181Cu, kLut1 = 0x0004080Cu, kTop = 0x80808080u;
+  const uint32_t even = w & 0x07070707u, odd = (w >> 4) & 0x07070707u;
+  const uint32_t be = __builtin_amdgcn_perm(kLut1, kLut0, even) | ((w << 4) & kTop);
+  const uint32_t bo = __builtin_amdgcn_perm(kLut1, kLut0, odd) | (w & kTop);
+  uint32_t v[4] = {__builtin_amdgcn_perm(0u, be, 0x020C000Cu), __builtin_amdgcn_perm(0u, bo, 0x020C000Cu),
+                   be & 0xFF00FF00u, bo & 0xFF00FF00u};
   if constexpr (K > 0) {
-    zero = (w & 0x77777777u) + 0x11111111u;
+    // bytes of ones where the code is not zero, spread over the halves
+    const uint32_t me = __builtin_amdgcn_perm(0x00FFFFFFu, 0xFFFFFFFFu, even);
+    const uint32_t mo = __builtin_amdgcn_perm(0x00FFFFFFu, 0xFFFFFFFFu, odd);
+    const uint32_t keep[4] = {__builtin_amdgcn_perm(0u, me, 0x02020000u), __builtin_amdgcn_perm(0u, mo, 0x02020000u),
+                              __builtin_amdgcn_perm(0u, me, 0x03030101u), __builtin_amdgcn_perm(0u, mo, 0x03030101u)};
+    uint32_t j = spread_nibbles(planes[0]);  // nibble n: element n's mantissa
 #pragma unroll
-    for (int b = 0; b < K; ++b) pl[b] = (planes[b] & 0xFu) | ((planes[b] << 12) & 0xF0000u);
-  }
-  uint32_t v[4];
+    for (int b = 1; b < K; ++b) j |= spread_nibbles(planes[b]) << b;
+    constexpr uint32_t kField = (((1u << K) - 1) << (10 - K)) * 0x10001u;
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    v[n] = (n < 3 ? nx << (n < 3 ? 10 - 4 * n : 0) : nx >> 2) & 0x1C001C00u;
-    if constexpr (K > 0) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int b = 0; b < K; ++b) m |= ((pl[b] >> n) & 0x00010001u) << (10 - K + b);
-      const uint32_t z = (zero >> (4 * n + 3)) & 0x00010001u;
-      v[n] |= m & ~((z << 10) - z);
+    for (int n = 0; n < 4; ++n) {
+      const int sh = 10 - K - 4 * n;
+      const uint32_t m = sh >= 0 ? j << (sh >= 0 ? sh : 0) : j >> (sh < 0 ? -sh : 0);
+      v[n] |= m & (kField & keep[n]);
     }
-    v[n] |= (w << (12 - 4 * n)) & 0x80008000u;
   }
   return __builtin_bit_cast(half8, make_uint4(v[0], v[1], v[2], v[3]));
 }

@@ -114,11 +114,11 @@ __device__ __forceinline__ EncodedKey encode_key(const uint4& raw, int lane, con
 // that are not `there` are not written. Every lane of the wave takes part.
 template <int K>
 __device__ __forceinline__ void store_key(const PagedAppendArgs& a, const CutBits& cut, const uint4& raw,
-                                          int64_t row8, int u, int lane, bool there) {
+                                          int row8, int u, int lane, bool there) {
   const EncodedKey e = a.hadamard ? encode_key<K, true>(raw, lane, cut) : encode_key<K, false>(raw, lane, cut);
   if (!there) return;
   const int g = lane & 7;
-  const int64_t row = row8 * 8 + u;
+  const int64_t row = (int64_t)row8 * 8 + u;
   *reinterpret_cast<uint32_t*>(a.pages.codes_se + row * (kDim / 2) + 4 * g) = e.word;
   if constexpr (K > 0) {
     if ((g & 3) < K)
@@ -127,11 +127,11 @@ __device__ __forceinline__ void store_key(const PagedAppendArgs& a, const CutBit
   if (g == 0) a.pages.key_scale[row] = e.scale;
 }
 // whole: the wave's 8 rows are the 8 tokens of one group, in order (uniform).
-__device__ __forceinline__ void store_value(const PagedAppendArgs& a, const uint4& raw, int64_t row8, int u,
+__device__ __forceinline__ void store_value(const PagedAppendArgs& a, const uint4& raw, int row8, int u,
                                             int lane, bool there, bool whole) {
   const int g = lane & 7;
   if (a.value_format == POT_VALUES_INT4) {
-    uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
+    uint8_t* rec = a.pages.values + (int64_t)row8 * kI4GroupBytes;
     if (whole) {
       store_record(raw, rec, lane, true, 0, 0, 0);
       return;
@@ -148,7 +148,7 @@ __device__ __forceinline__ void store_value(const PagedAppendArgs& a, const uint
     return;
   }
   if (!there) return;
-  uint16_t* at = reinterpret_cast<uint16_t*>(a.pages.values) + row8 * (8 * kDim) + 64 * g + u;
+  uint16_t* at = reinterpret_cast<uint16_t*>(a.pages.values) + (int64_t)row8 * (8 * kDim) + 64 * g + u;
   const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -159,7 +159,7 @@ __device__ __forceinline__ void store_value(const PagedAppendArgs& a, const uint
 
 // The group of cache rows of a token for kv head 0 (-1: its page is not there); a kv head's
 // stands page_groups further on.
-__device__ __forceinline__ int64_t token_row8(const PagesArg& p, const Token& t) {
+__device__ __forceinline__ int token_row8(const PagesArg& p, const Token& t) {
   return t.b < 0 || t.place < 0 ? -1 : group_row8(p, p.table + (int64_t)t.b * p.table_len, 0, t.place >> 3);
 }
 
@@ -198,12 +198,11 @@ __global__ __launch_bounds__(kBlock) void paged_append_tokens_kernel(const Paged
   float* my_part = part + (MODE == kHalves ? (wave * 8 + row) * kPartStride : 0);
   const CutBits cut = cut_bits(a.tab);
   const int qk_end = n.Hq + n.Hkv;
-  const int64_t row8 = h_end > n.Hq ? token_row8(a.pages, t) : -1;
+  const int row8 = h_end > n.Hq ? token_row8(a.pages, t) : -1;
   const int u = t.place & 7;
   // the wave's rows are a group's 8 tokens: each lane's group is its neighbour row's, and its
   // place in it is the row
-  const int64_t first8 = ((int64_t)__builtin_amdgcn_readfirstlane((int)(row8 >> 32)) << 32) |
-                         (uint32_t)__builtin_amdgcn_readfirstlane((int)row8);
+  const int first8 = __builtin_amdgcn_readfirstlane(row8);
   const bool whole = __all(row8 >= 0 && row8 == first8 && u == row);
   const bool turns = n.rot_dim > 0 && h_first < qk_end;
   Turn<MODE> turn{};
@@ -238,10 +237,10 @@ __global__ __launch_bounds__(kBlock) void paged_append_tokens_kernel(const Paged
     });
   part_of(n.k, n.k_weight, n.Hq, n.Hkv, [&](int h, float (&x)[8]) {
     if (turns) rotate_row<MODE>(x, turn, n.rot_dim, g, my_part);
-    store_key<K>(a, cut, natural_halves<MODE>(x), row8 + (int64_t)h * a.pages.page_groups, u, lane, row8 >= 0);
+    store_key<K>(a, cut, natural_halves<MODE>(x), row8 + h * a.pages.page_groups, u, lane, row8 >= 0);
   });
   part_of(n.v, nullptr, qk_end, n.Hkv, [&](int h, float (&x)[8]) {
-    store_value(a, natural_halves<MODE>(x), row8 + (int64_t)h * a.pages.page_groups, u, lane, row8 >= 0, whole);
+    store_value(a, natural_halves<MODE>(x), row8 + h * a.pages.page_groups, u, lane, row8 >= 0, whole);
   });
 }
 
@@ -292,7 +291,7 @@ __global__ __launch_bounds__(64) void paged_append_heads_kernel(const PagedAppen
   if (__any(there && kind == 0))
     store_row<MODE, false>(n.q_out, ((int64_t)tok * n.Hq + hh) * kDim, g, n.q_out_dtype, x, there && kind == 0);
   if (!__any(there && kind != 0)) return;
-  const int64_t first = token_row8(a.pages, t), row8 = first + (int64_t)hh * a.pages.page_groups;
+  const int first = token_row8(a.pages, t), row8 = first + hh * a.pages.page_groups;
   const uint4 halves = natural_halves<MODE>(x);
   if (__any(there && kind == 1))
     store_key<K>(a, cut_bits(a.tab), halves, row8, t.place & 7, lane, there && kind == 1 && first >= 0);

@@ -6,8 +6,11 @@
 // queries as fp16 integers: exact sums), rows of K in such an order that a lane ends up with
 // the scores of one query and 8 consecutive keys of either half tile, which are then the
 // operand of O^T = V^T P^T as they stand; a query's reference, sum and outputs are its lanes'
-// own, so a rise of the reference is 16 products a lane. Weights go in as fp16 numbers and what
-// rounding left of them. The reference rises only when a weight would leave fp16's range.
+// own, so a rise of the reference is 16 products a lane. The reference rises only when a weight
+// would leave fp16's range.
+//
+// Tiles that every query sees in full take a loop without a test of keys; the others (the
+// sequence's end, the window's, pages that are not there) go through the same code with them.
 #pragma once
 
 #include "paged.hpp"
@@ -25,8 +28,17 @@ struct FewValues<POT_VALUES_INT4> {
   uint4 f[2], s[2], z[2];
 };
 
-template <int K, int VF>
-__global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(const PagedAttendArgs a) {
+// Value of lane `from` (any lane).
+__device__ __forceinline__ int lane_value(int v, int from) {
+  return __builtin_amdgcn_ds_bpermute(from << 2, v);
+}
+
+// UNI: a tile lies in one page (page sizes of whole tiles). LOW: the weights' rounding goes into
+// the products too (outputs of 32 bits).
+template <int K, int VF, bool UNI, bool LOW>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
+    few_simd_waves(K, UNI))))
+void paged_few_kernel(const PagedAttendArgs a) {
   constexpr int NW = kFewWaves, R = kFewRows;
   __shared__ uint4 sq[R][8];
   __shared__ float sc[R], sm[NW][R], sl[NW][R];
@@ -42,70 +54,66 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(const PagedAt
   const int32_t* table = a.pages.table + (int64_t)b * a.pages.table_len;
   const int col = lane & 15, grp = lane >> 4;
 
+  // The rows of a tile's groups: of the first one (UNI, uniform), or of group lane % 8 in each
+  // lane; -1 where there is no page. Tiles past the run: the last one again.
+  auto rows_of = [&](int j) -> int {
+    const int g = tile_start(seen, min(j, run.end - 1)) / 8;
+    return group_row8(a.pages, table, kvh, UNI ? g : g + (lane & 7));
+  };
+  // Row of group g (0 .. 7, by lane) of a tile; groups without a page read row 0, which is there.
+  auto row_at = [&](int rows8, int g) -> int64_t {
+    return UNI ? max(rows8, 0) + g : max(lane_value(rows8, g), 0);
+  };
+
   // a wave's loads of a tile: codes of keys 32 kb + 8 (col / 4) + 4 s + col % 4, dimensions
   // 16 grp ..+15; scales and values of keys 32 kb + 8 grp ..+7
   uint2 kc[2][2];
   uint32_t kp[2][2][K > 0 ? K : 1];
   float4 ks[2][2];
   FewValues<VF> vr;
-  bool there[2];
-  auto load_keys = [&](int j) {
-    const int g0 = tile_start(seen, j) / 8;
+  auto load_keys = [&](int rows8) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const int g = g0 + 4 * kb + (col >> 2);
-      const int64_t row8 = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
+      const int64_t row = row_at(rows8, 4 * kb + (col >> 2)) * 8 + (col & 3);
+      const uint8_t* c = a.pages.codes_se + row * 32 + 8 * grp;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        kc[kb][s] = make_uint2(0u, 0u);
+      for (int s = 0; s < 2; ++s) kc[kb][s] = *reinterpret_cast<const uint2*>(c + 128 * s);
+      if constexpr (K > 0) {
+        const uint8_t* m = a.pages.codes_m + row * 8 * K + 2 * grp;
 #pragma unroll
-        for (int p = 0; p < K; ++p) kp[kb][s][p] = 0u;
-        if (row8 >= 0) {
-          const int64_t row = row8 * 8 + 4 * s + (col & 3);
-          kc[kb][s] = *reinterpret_cast<const uint2*>(a.pages.codes_se + row * 32 + 8 * grp);
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int p = 0; p < K; ++p)
-            kp[kb][s][p] = *reinterpret_cast<const uint16_t*>(a.pages.codes_m + row * 8 * K + 8 * p + 2 * grp);
-        }
+            kp[kb][s][p] = *reinterpret_cast<const uint16_t*>(m + 32 * K * s + 8 * p);
       }
     }
   };
-  auto load_values = [&](int j) {
-    const int g0 = tile_start(seen, j) / 8;
+  auto load_values = [&](int rows8) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const int g = g0 + 4 * kb + grp;
-      const int64_t row8 = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
-      there[kb] = row8 >= 0;
-      const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-      ks[kb][0] = ks[kb][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      const int64_t row8 = row_at(rows8, 4 * kb + grp);
+      const float4* sp = reinterpret_cast<const float4*>(a.pages.key_scale + row8 * 8);
+      ks[kb][0] = sp[0];
+      ks[kb][1] = sp[1];
       if constexpr (VF == POT_VALUES_INT4) {
-        vr.f[kb] = vr.s[kb] = vr.z[kb] = none;
+        const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
+        vr.f[kb] = *reinterpret_cast<const uint4*>(rec + 16 * col);
+        vr.s[kb] = *reinterpret_cast<const uint4*>(rec + kI4Steps);
+        vr.z[kb] = *reinterpret_cast<const uint4*>(rec + kI4Minima);
       } else {
+        const uint8_t* v = a.pages.values + row8 * (16 * kDim) + 16 * col;
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb) vr.f[kb][nb] = none;
-      }
-      if (row8 >= 0) {
-        const float4* sp = reinterpret_cast<const float4*>(a.pages.key_scale + row8 * 8);
-        ks[kb][0] = sp[0];
-        ks[kb][1] = sp[1];
-        if constexpr (VF == POT_VALUES_INT4) {
-          const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
-          vr.f[kb] = *reinterpret_cast<const uint4*>(rec + 16 * col);
-          vr.s[kb] = *reinterpret_cast<const uint4*>(rec + kI4Steps);
-          vr.z[kb] = *reinterpret_cast<const uint4*>(rec + kI4Minima);
-        } else {
-#pragma unroll
-          for (int nb = 0; nb < 4; ++nb)
-            vr.f[kb][nb] = *reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim) + 256 * nb + 16 * col);
-        }
+        for (int nb = 0; nb < 4; ++nb) vr.f[kb][nb] = *reinterpret_cast<const uint4*>(v + 256 * nb);
       }
     }
   };
   int j = run.first + wave;
+  int rows_now = -1, rows_next = -1;
   if (j < run.end) {
-    load_keys(j);
-    load_values(j);
+    rows_now = rows_of(j);
+    load_keys(rows_now);
+    load_values(rows_now);
+    rows_next = rows_of(j + NW);
   }
 
   if (wave < R / 8) {
@@ -124,14 +132,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(const PagedAt
 #pragma unroll
   for (int s = 0; s < 2; ++s) q[s] = __builtin_bit_cast(half8, sq[col][2 * grp + s]);
   const float c = sc[col];
-  const int place = p_first + (col < rows ? col : 0) / a.G;
 
   f32x4 acc[4];
 #pragma unroll
   for (int nb = 0; nb < 4; ++nb) acc[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, l = 0.0f;
-  while (j < run.end) {
-    const int t0 = tile_start(seen, j);
+
+  auto tile = [&](auto part_tag, int t0) {
+    constexpr bool PART = decltype(part_tag)::value;
     float y[2][8];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -142,31 +150,44 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(const PagedAt
         for (int h = 0; h < 2; ++h) {
           uint32_t pl[K > 0 ? K : 1];
 #pragma unroll
-          for (int p = 0; p < K; ++p) pl[p] = kp[kb][s][p] >> (8 * h);
+          for (int p = 0; p < K; ++p) pl[p] = h ? kp[kb][s][p] >> 8 : kp[kb][s][p] & 0xFFu;
           d = __builtin_amdgcn_mfma_f32_16x16x32_f16(paged_weights<K>(h ? kc[kb][s].y : kc[kb][s].x, pl),
                                                      q[h], d, 0, 0, 0);
         }
-        const float4 sv = ks[kb][s];
-        y[kb][4 * s] = d[0] * sv.x;
-        y[kb][4 * s + 1] = d[1] * sv.y;
-        y[kb][4 * s + 2] = d[2] * sv.z;
-        y[kb][4 * s + 3] = d[3] * sv.w;
-      }
-    const int jn = j + NW;
-    if (jn < run.end) load_keys(jn);
-    const bool part = !all_seen(p_first, p_last, t0, a.window, a.n_sink) || __any(!there[0] || !there[1]);
-    if (part) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+        for (int i = 0; i < 4; ++i) y[kb][4 * s + i] = d[i];
+      }
+    // the codes have become operands: the next tile's may come
+    const int rows_tile = rows_now;
+    load_keys(rows_next);
+    rows_now = rows_next;
+    rows_next = rows_of(j + 2 * NW);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const float4 sv = ks[kb][s];
+        y[kb][4 * s] *= sv.x;
+        y[kb][4 * s + 1] *= sv.y;
+        y[kb][4 * s + 2] *= sv.z;
+        y[kb][4 * s + 3] *= sv.w;
+      }
+    bool there[2] = {true, true};
+    if constexpr (PART) {
+      const int place = p_first + (col < rows ? col : 0) / a.G;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        there[kb] = (UNI ? rows_tile : lane_value(rows_tile, 4 * kb + grp)) >= 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int key = t0 + 32 * kb + 8 * grp + i;
           if (!(there[kb] && key < seen.end && sees(place, key, a.window, a.n_sink))) y[kb][i] = -INFINITY;
         }
+      }
     }
-    float top = y[0][0];
+    float top = fmaxf(y[0][0], y[0][1]);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, y[i >> 3][i & 7]);
+    for (int i = 2; i < 16; ++i) top = fmaxf(top, y[i >> 3][i & 7]);
     const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
@@ -180,57 +201,75 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(const PagedAt
       m = to;
     }
     uint32_t hi[2][4], lo[2][4];
+    half8 seen_ones[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       float p[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = paged_weight(y[kb][i], m, c);
-      if (part) {
+      if constexpr (PART) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = y[kb][i] == -INFINITY ? 0.0f : p[i];
+        for (int i = 0; i < 8; ++i) {
+          const bool off = y[kb][i] == -INFINITY;
+          p[i] = off ? 0.0f : p[i];
+          seen_ones[kb][i] = off ? (_Float16)0.0f : (_Float16)1.0f;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         l += p[2 * i];
         l += p[2 * i + 1];
         hi[kb][i] = pack_half(p[2 * i], p[2 * i + 1]);
-        lo[kb][i] = low_part(p[2 * i], p[2 * i + 1], hi[kb][i]);
+        if constexpr (LOW) lo[kb][i] = low_part(p[2 * i], p[2 * i + 1], hi[kb][i]);
       }
     }
-    auto fragment = [&](int kb, int nb) -> half8 {
-      uint4 v;
-      if constexpr (VF == POT_VALUES_INT4) {
-        const uint4 w = vr.f[kb];
-        const uint32_t w0 = nb < 2 ? w.x : w.z, w1 = nb < 2 ? w.y : w.w;
-        v = int4_values((nb & 1 ? w0 >> 4 : w0) & 0x0F0F0F0Fu, (nb & 1 ? w1 >> 4 : w1) & 0x0F0F0F0Fu,
-                        vr.s[kb], vr.z[kb]);
-      } else {
-        v = vr.f[kb][nb];
-      }
-      return __builtin_bit_cast(half8, part ? mask_tokens(v, t0 + 32 * kb + 8 * grp, seen.end) : v);
-    };
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[kb][0], hi[kb][1], hi[kb][2], hi[kb][3]));
-      const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[kb][0], lo[kb][1], lo[kb][2], lo[kb][3]));
+      half8 pl{};
+      if constexpr (LOW) pl = __builtin_bit_cast(half8, make_uint4(lo[kb][0], lo[kb][1], lo[kb][2], lo[kb][3]));
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb) {
-        half8 v = fragment(kb, nb);
-        if (part && __any(has_special(__builtin_bit_cast(uint4, v)))) {
-          half8 marks, ones;
-          split_special(v, &v, &marks);
+        uint4 u;
+        if constexpr (VF == POT_VALUES_INT4) {
+          const uint4 w = vr.f[kb];
+          const uint32_t w0 = nb < 2 ? w.x : w.z, w1 = nb < 2 ? w.y : w.w;
+          u = int4_values((nb & 1 ? w0 >> 4 : w0) & 0x0F0F0F0Fu, (nb & 1 ? w1 >> 4 : w1) & 0x0F0F0F0Fu,
+                          vr.s[kb], vr.z[kb]);
+        } else {
+          u = vr.f[kb][nb];
+        }
+        if constexpr (PART) u = mask_tokens(u, t0 + 32 * kb + 8 * grp, there[kb] ? seen.end : 0);
+        half8 v = __builtin_bit_cast(half8, u);
+        if constexpr (PART) {
+          if (__any(has_special(u))) {
+            half8 marks;
+            split_special(v, &v, &marks);
+            const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(marks, seen_ones[kb], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) ones[i] = y[kb][i] == -INFINITY ? (_Float16)0.0f : (_Float16)1.0f;
-          const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(marks, ones, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[nb][i] += special_sum(n[i]);
+            for (int i = 0; i < 4; ++i) acc[nb][i] += special_sum(n[i]);
+          }
         }
         acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph, acc[nb], 0, 0, 0);
-        acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, acc[nb], 0, 0, 0);
+        if constexpr (LOW) acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, acc[nb], 0, 0, 0);
       }
     }
-    if (jn < run.end) load_values(jn);
-    j = jn;
+    load_values(rows_now);
+    j += NW;
+  };
+#pragma nounroll
+  while (j < run.end) {
+    int t0 = tile_start(seen, j);
+    auto whole = [&]() {
+      return all_seen(p_first, p_last, t0, a.window, a.n_sink) && (UNI ? rows_now >= 0 : __all(rows_now >= 0));
+    };
+#pragma nounroll
+    while (whole()) {
+      tile(std::false_type{}, t0);
+      if (j >= run.end) break;
+      t0 = tile_start(seen, j);
+    }
+    if (j < run.end) tile(std::true_type{}, t0);
   }
 
   // ---- the waves' sums -------------------------------------------------------------------
@@ -276,9 +315,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(const PagedAt
 
 template <int K, int VF>
 hipError_t launch_few(const PagedAttendArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_few_kernel<K, VF>),
-                     dim3((uint32_t)a.plan.few_splits, (uint32_t)a.pages.Hkv, (uint32_t)a.packed.B),
-                     dim3(64 * kFewWaves), 0, stream, a);
+  const dim3 grid((uint32_t)a.plan.few_splits, (uint32_t)a.pages.Hkv, (uint32_t)a.packed.B);
+  const bool uni = a.pages.page_groups % (kWTile / 8) == 0;
+  if (a.out_dtype == POT_FP32) {
+    if (uni) hipLaunchKernelGGL((paged_few_kernel<K, VF, true, true>), grid, dim3(64 * kFewWaves), 0, stream, a);
+    else hipLaunchKernelGGL((paged_few_kernel<K, VF, false, true>), grid, dim3(64 * kFewWaves), 0, stream, a);
+  } else {
+    if (uni) hipLaunchKernelGGL((paged_few_kernel<K, VF, true, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
+    else hipLaunchKernelGGL((paged_few_kernel<K, VF, false, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
+  }
   return hipGetLastError();
 }
 

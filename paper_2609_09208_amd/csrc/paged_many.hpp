@@ -134,22 +134,22 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
       const int g = g0 + wave + NW * i;
-      const int64_t row8 = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
+      const int row8 = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
       st_there[i] = row8 >= 0;
       st[i] = ManyStage<VF>{};
       if (row8 >= 0) {
-        const int64_t row = row8 * 8 + (lane >> 3);
+        const int64_t row = (int64_t)row8 * 8 + (lane >> 3);
         st[i].code = *reinterpret_cast<const uint32_t*>(a.pages.codes_se + row * 32 + 4 * (lane & 7));
 #pragma unroll
         for (int p = 0; p < K; ++p) st[i].plane[p] = a.pages.codes_m[row * 8 * K + 8 * p + (lane & 7)];
-        if (lane < 8) st[i].scale = a.pages.key_scale[row8 * 8 + lane];
+        if (lane < 8) st[i].scale = a.pages.key_scale[(int64_t)row8 * 8 + lane];
         if constexpr (VF == POT_VALUES_INT4) {
-          const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
+          const uint8_t* rec = a.pages.values + (int64_t)row8 * kI4GroupBytes;
           st[i].n = *reinterpret_cast<const uint2*>(rec + 16 * (lane & 15) + 8 * (lane >> 5));
           st[i].s = *reinterpret_cast<const uint4*>(rec + kI4Steps);
           st[i].z = *reinterpret_cast<const uint4*>(rec + kI4Minima);
         } else {
-          st[i].v = *reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim) + 16 * lane);
+          st[i].v = *reinterpret_cast<const uint4*>(a.pages.values + (int64_t)row8 * (16 * kDim) + 16 * lane);
         }
       }
     }

@@ -226,6 +226,9 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
 
 // Rows (new token x query head of a kv head) that the kernel of few rows takes of a sequence.
 constexpr int kFewRows = 16;
+// Waves per SIMD that the kernel of few rows leaves registers for; its workgroups have four waves, so as
+// many to a CU. uni: pages of whole tiles.
+constexpr int few_simd_waves(int mant_bits, bool uni) { return mant_bits == 0 && uni ? 4 : 3; }
 // How a call is split: the kernel of few rows in few_splits key ranges, the kernel of many in
 // tiles of 32 many_waves rows and many_splits ranges; splits of 0: not launched. Sequences of up
 // to few_limit rows go to the former.
