@@ -38,6 +38,10 @@ __device__ __forceinline__ void load8(const void* base, int64_t at, int chunk, i
   else to_floats<POT_FP16, kNeighbours>(load_row<POT_FP16, kNeighbours>(base, at, chunk), x);
 }
 
+// Weights, references and factors (Reference).
+constexpr float kWeightShift = 7.0f, kMostWeight = 15.0f, kNoReference = -3e38f, kLeastFactor = 1e-30f;
+constexpr float kFarReference = 0x1p20f;  // fp32's steps there are 1/8
+
 // Walsh-Hadamard rotation of a row over its 8 lanes (lane g: elements 8g .. 8g + 7), fp64
 // stages of span 1 .. 32, one rounding to fp32.
 __device__ __forceinline__ void rotate_hadamard(float (&x)[8], int lane) {
@@ -76,7 +80,7 @@ __device__ __forceinline__ uint4 quantised_query(float (&x)[8], int hadamard, in
   const float inv = 127.0f / top;  // correctly rounded divisions
 #pragma unroll
   for (int i = 0; i < 8; ++i) q[i] = top == 0.0f ? 0 : quantize_int8(x[i], inv);
-  *factor = __fmul_rn(top / 127.0f, log2e_f32()) * 32.0f;
+  *factor = fmaxf(__fmul_rn(top / 127.0f, log2e_f32()) * 32.0f, kLeastFactor);
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = pack_half((float)q[i], (float)q[i + 4]);
@@ -151,34 +155,64 @@ __device__ __forceinline__ uint4 mask_tokens(uint4 v, int first, int end) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Values that are infinite or NaN, in tiles of which some query sees a part only: their product
-// with a weight of 0 would be NaN where they are not seen. They go into the sums as 0, and
-// beside those the matrix cores count them for the keys that a query sees.
-__device__ __forceinline__ bool has_special(const uint4& v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    any |= (w[i] & 0x7C00u) == 0x7C00u || (w[i] & 0x7C000000u) == 0x7C000000u;
-  return any;
+// Which of a tile's keys a query sees, t0 the tile's first: key t0 + e is seen if e <= last and
+// (e > before or e < sinks).
+struct SeenKeys {
+  int last, before, sinks;
+};
+__device__ __forceinline__ SeenKeys seen_keys(const PagedAttendArgs& a, int place, int end, int t0) {
+  return {min(place, end - 1) - t0, a.window > 0 ? place - a.window - t0 : -1, a.n_sink - t0};
 }
-__device__ __forceinline__ void split_special(const half8& v, half8* rest, half8* marks) {
-  const uint4 u = __builtin_bit_cast(uint4, v);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w}, kOne = 0x3C003C00u;
-  uint32_t r[4], m[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t off = ((w[i] & 0x7C00u) == 0x7C00u ? 0x0000FFFFu : 0u) |
-                         ((w[i] & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
-    r[i] = w[i] & ~off;
-    m[i] = kOne & off;
-  }
-  *rest = __builtin_bit_cast(half8, make_uint4(r[0], r[1], r[2], r[3]));
-  *marks = __builtin_bit_cast(half8, make_uint4(m[0], m[1], m[2], m[3]));
+__device__ __forceinline__ bool is_seen(const SeenKeys& s, int e) {
+  return e <= s.last && (e > s.before || e < s.sinks);
+}
+// The same of keys e0 .. e0 + 7 as bits.
+__device__ __forceinline__ uint32_t seen_bits(const SeenKeys& s, int e0) {
+  auto below = [](int n) { return (1u << min(max(n, 0), 8)) - 1u; };  // keys of the 8 before the n-th
+  return below(s.last + 1 - e0) & (~below(s.before + 1 - e0) | below(s.sinks - e0)) & 0xFFu;
+}
+// y where bit e of the mask is set, minus infinity elsewhere.
+__device__ __forceinline__ float if_seen(float y, uint32_t mask, int e) {
+  const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)mask, e, 1);
+  return __uint_as_float((__float_as_uint(y) & all) | (0xFF800000u & ~all));
+}
+
+// Values that are infinite or NaN, in tiles of which some query sees a part only: their product
+// with a weight of 0 would be NaN where they are not seen. They go into the sums as 0; after the
+// last tile, the matrix cores count them for the keys that a query sees (a path that no ordinary
+// cache takes: it reads the values again).
+__device__ __forceinline__ uint32_t special_mask(uint32_t w) {
+  return ((w & 0x7C00u) == 0x7C00u ? 0x0000FFFFu : 0u) | ((w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
+}
+__device__ __forceinline__ bool has_special(const uint4& v) {
+  return (special_mask(v.x) | special_mask(v.y) | special_mask(v.z) | special_mask(v.w)) != 0;
+}
+__device__ __forceinline__ uint4 without_special(const uint4& v) {
+  return make_uint4(v.x & ~special_mask(v.x), v.y & ~special_mask(v.y), v.z & ~special_mask(v.z),
+                    v.w & ~special_mask(v.w));
+}
+__device__ __forceinline__ half8 special_marks(const uint4& v) {  // 1 where a value is special
+  constexpr uint32_t kOne = 0x3C003C00u;
+  return __builtin_bit_cast(half8, make_uint4(kOne & special_mask(v.x), kOne & special_mask(v.y),
+                                              kOne & special_mask(v.z), kOne & special_mask(v.w)));
 }
 // What the counted values make of a sum.
 __device__ __forceinline__ float special_sum(float count) {
   return count > 0.0f ? __builtin_nanf("") : 0.0f;
+}
+// The fp16 values of dimension d of the 8 tokens of a group of cache rows.
+template <int VF>
+__device__ __forceinline__ uint4 group_values(const PagesArg& p, int row8, int d) {
+  if constexpr (VF == POT_VALUES_INT4) {
+    const uint8_t* rec = p.values + (int64_t)row8 * kI4GroupBytes;
+    const uint2 n = *reinterpret_cast<const uint2*>(rec + 16 * (d & 15) + 8 * (d >> 5));
+    const int sh = (d & 16) ? 4 : 0;
+    return int4_values((n.x >> sh) & 0x0F0F0F0Fu, (n.y >> sh) & 0x0F0F0F0Fu,
+                       *reinterpret_cast<const uint4*>(rec + kI4Steps),
+                       *reinterpret_cast<const uint4*>(rec + kI4Minima));
+  } else {
+    return *reinterpret_cast<const uint4*>(p.values + (int64_t)row8 * (16 * kDim) + 16 * d);
+  }
 }
 
 // Weights of fp32 as fp16 operands: rounded to nearest, and what that left, rounded in turn.
@@ -203,18 +237,56 @@ __device__ __forceinline__ void store_out1(void* out, int64_t at, int type, floa
   else static_cast<uint16_t*>(out)[at] = (uint16_t)pack_half(a, a);
 }
 
-// A key's weight: y its sum times its scale, m the query's reference, c its factor. Weights are
-// formed as 2^(x - m + 7) and the reference rises once a key is more than 2^8 over it, so the
-// largest of a query's lies between 2^7 and 2^15 and fp16's normal numbers reach 2^-21 of it at
-// the least.
-constexpr float kWeightShift = 7.0f, kMostRise = 8.0f;
-__device__ __forceinline__ float paged_weight(float y, float m, float c) {
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(y - m, c, kWeightShift));
+// A query's reference m (a sum times its scale), and b = 7 - m c as rounded: a key's weight is
+// 2^(y c + b), y its sum times its scale, c the query's factor. What b's rounding leaves is the
+// same for all weights, and a new reference takes the old sums with it by 2^(b - b_old), so it
+// does not matter, until b is so large that a weight of 2^7 could leave fp16's range: then the
+// difference y - m is taken first (far, for a wave).
+//
+// The reference rises, to a tile's largest y, when that key's weight would be over 2^15; it is
+// 2^7 then, so fp16's normal numbers reach 2^-21 of the largest weight at the least. A key that is
+// not seen has y = minus infinity and weight 0: factors are at least kLeastFactor, and b is 0 as
+// long as there is no reference.
+struct Reference {
+  float m = kNoReference, b = 0.0f;
+  bool far = false;  // uniform
+};
+// y as weight_of takes it.
+template <int N>
+__device__ __forceinline__ void far_sums(const Reference& r, float (&y)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] -= r.m;
 }
-
-// 2^((m - M) c) of two references (-inf: nothing summed yet), c >= 0.
+__device__ __forceinline__ float weight_shift(const Reference& r) { return r.far ? kWeightShift : r.b; }
+__device__ __forceinline__ float weight_of(float y, float c, float shift) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(y, c, shift));
+}
+// Whether the reference has to rise for a largest y of `top` (or there is none), for the wave.
+__device__ __forceinline__ bool must_rise(const Reference& r, float top, float c) {
+  const float x = r.far ? __builtin_fmaf(top - r.m, c, kWeightShift) : __builtin_fmaf(top, c, r.b);
+  return __any(x > kMostWeight || r.m == kNoReference);
+}
+// 2^((m - M) c) of two references.
 __device__ __forceinline__ float between(float m, float M, float c) {
-  return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - M) * c);
+  return __builtin_amdgcn_exp2f((m - M) * c);
+}
+// Raises the reference to `top`, the largest y of the query in the tile; returns what the sums
+// are to be multiplied by.
+__device__ __forceinline__ float raise(Reference& r, float top, float c) {
+  const float to = fmaxf(r.m, top);
+  const float b = to == kNoReference ? 0.0f : __builtin_fmaf(-to, c, kWeightShift);
+  const bool far = r.far || __any(fabsf(b) >= kFarReference);
+  float f = r.far ? (r.m - to) * c : far ? __builtin_fmaf(-to, c, kWeightShift - r.b) : b - r.b;
+  f = r.m == kNoReference ? 0.0f : __builtin_amdgcn_exp2f(f);
+  r.m = to;
+  r.b = b;
+  r.far = far;
+  return f;
+}
+// What takes sums to the weights 2^(y c - m c + 7) of the exact reference, for a merge with others.
+__device__ __forceinline__ float exact_reference(const Reference& r, float c) {
+  return r.far || r.m == kNoReference
+             ? 1.0f : __builtin_amdgcn_exp2f(-__builtin_fmaf(r.m, c, r.b - kWeightShift));
 }
 
 }  // namespace potattn

@@ -13,7 +13,7 @@ __global__ __launch_bounds__(256) void paged_few_merge_kernel(const PagedAttendA
   if (r >= t.n * a.G) return;
   const float* part = a.few_part + (((int64_t)b * a.pages.Hkv + kvh) * S * kFewRows + r) * kPartial;
   constexpr int kNext = kFewRows * kPartial;
-  float M = -INFINITY;
+  float M = kNoReference;
   for (int s = 0; s < S; ++s) M = fmaxf(M, part[(int64_t)s * kNext + kDim]);
   float L = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};

@@ -6,7 +6,7 @@
 // queries as fp16 integers: exact sums), rows of K in such an order that a lane ends up with
 // the scores of one query and 8 consecutive keys of either half tile, which are then the
 // operand of O^T = V^T P^T as they stand; a query's reference, sum and outputs are its lanes'
-// own, so a rise of the reference is 16 products a lane. The reference rises only when a weight
+// own, so a rise of the reference is 16 products a lane. The reference rises only when weights
 // would leave fp16's range.
 //
 // Tiles that every query sees in full take a loop without a test of keys; the others (the
@@ -136,7 +136,11 @@ void paged_few_kernel(const PagedAttendArgs a) {
   f32x4 acc[4];
 #pragma unroll
   for (int nb = 0; nb < 4; ++nb) acc[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = -INFINITY, l = 0.0f;
+  Reference ref;
+  float l = 0.0f;
+
+  auto place_of_col = [&]() { return p_first + (col < rows ? col : 0) / a.G; };
+  bool special = false;  // a tile in part held special values (paged.hpp)
 
   auto tile = [&](auto part_tag, int t0) {
     constexpr bool PART = decltype(part_tag)::value;
@@ -172,17 +176,16 @@ void paged_few_kernel(const PagedAttendArgs a) {
         y[kb][4 * s + 2] *= sv.z;
         y[kb][4 * s + 3] *= sv.w;
       }
-    bool there[2] = {true, true};
+    int end[2] = {0, 0};
     if constexpr (PART) {
-      const int place = p_first + (col < rows ? col : 0) / a.G;
+      const SeenKeys sk = seen_keys(a, place_of_col(), seen.end, t0 + 8 * grp);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        there[kb] = (UNI ? rows_tile : lane_value(rows_tile, 4 * kb + grp)) >= 0;
+        const bool there = (UNI ? rows_tile : lane_value(rows_tile, 4 * kb + grp)) >= 0;
+        const uint32_t mask = there ? seen_bits(sk, 32 * kb) : 0u;
+        end[kb] = there ? seen.end : 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = t0 + 32 * kb + 8 * grp + i;
-          if (!(there[kb] && key < seen.end && sees(place, key, a.window, a.n_sink))) y[kb][i] = -INFINITY;
-        }
+        for (int i = 0; i < 8; ++i) y[kb][i] = if_seen(y[kb][i], mask, i);
       }
     }
     float top = fmaxf(y[0][0], y[0][1]);
@@ -192,37 +195,28 @@ void paged_few_kernel(const PagedAttendArgs a) {
     top = fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
-    const bool rises = top > m && (m == -INFINITY || (top - m) * c > kMostRise);
-    if (__any(rises)) {
-      const float to = rises ? top : m, f = between(m, to, c);
+    if (must_rise(ref, top, c)) {
+      const float f = raise(ref, top, c);
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb) acc[nb] *= f;
       l *= f;
-      m = to;
     }
+    if (ref.far) {  // uniform
+      far_sums(ref, y[0]);
+      far_sums(ref, y[1]);
+    }
+    const float shift = weight_shift(ref);
     uint32_t hi[2][4], lo[2][4];
-    half8 seen_ones[2];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = paged_weight(y[kb][i], m, c);
-      if constexpr (PART) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const bool off = y[kb][i] == -INFINITY;
-          p[i] = off ? 0.0f : p[i];
-          seen_ones[kb][i] = off ? (_Float16)0.0f : (_Float16)1.0f;
-        }
-      }
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        l += p[2 * i];
-        l += p[2 * i + 1];
-        hi[kb][i] = pack_half(p[2 * i], p[2 * i + 1]);
-        if constexpr (LOW) lo[kb][i] = low_part(p[2 * i], p[2 * i + 1], hi[kb][i]);
+        const float p0 = weight_of(y[kb][2 * i], c, shift), p1 = weight_of(y[kb][2 * i + 1], c, shift);
+        l += p0;
+        l += p1;
+        hi[kb][i] = pack_half(p0, p1);
+        if constexpr (LOW) lo[kb][i] = low_part(p0, p1, hi[kb][i]);
       }
-    }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[kb][0], hi[kb][1], hi[kb][2], hi[kb][3]));
@@ -239,17 +233,12 @@ void paged_few_kernel(const PagedAttendArgs a) {
         } else {
           u = vr.f[kb][nb];
         }
-        if constexpr (PART) u = mask_tokens(u, t0 + 32 * kb + 8 * grp, there[kb] ? seen.end : 0);
-        half8 v = __builtin_bit_cast(half8, u);
         if constexpr (PART) {
-          if (__any(has_special(u))) {
-            half8 marks;
-            split_special(v, &v, &marks);
-            const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(marks, seen_ones[kb], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[nb][i] += special_sum(n[i]);
-          }
+          u = mask_tokens(u, t0 + 32 * kb + 8 * grp, end[kb]);
+          special |= has_special(u);
+          u = without_special(u);
         }
+        const half8 v = __builtin_bit_cast(half8, u);
         acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph, acc[nb], 0, 0, 0);
         if constexpr (LOW) acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, acc[nb], 0, 0, 0);
       }
@@ -257,19 +246,43 @@ void paged_few_kernel(const PagedAttendArgs a) {
     load_values(rows_now);
     j += NW;
   };
+  auto whole = [&](int t0, int rows8) {
+    return all_seen(p_first, p_last, t0, a.window, a.n_sink) && (UNI ? rows8 >= 0 : __all(rows8 >= 0));
+  };
 #pragma nounroll
   while (j < run.end) {
     int t0 = tile_start(seen, j);
-    auto whole = [&]() {
-      return all_seen(p_first, p_last, t0, a.window, a.n_sink) && (UNI ? rows_now >= 0 : __all(rows_now >= 0));
-    };
 #pragma nounroll
-    while (whole()) {
+    while (whole(t0, rows_now)) {
       tile(std::false_type{}, t0);
       if (j >= run.end) break;
       t0 = tile_start(seen, j);
     }
     if (j < run.end) tile(std::true_type{}, t0);
+  }
+  if (__any(special)) {
+#pragma nounroll
+    for (j = run.first + wave; j < run.end; j += NW) {
+      const int t0 = tile_start(seen, j), rows8 = rows_of(j);
+      if (whole(t0, rows8)) continue;
+      const SeenKeys sk = seen_keys(a, place_of_col(), seen.end, t0 + 8 * grp);
+#pragma nounroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const int g = 4 * kb + grp, row8 = UNI ? (rows8 < 0 ? -1 : rows8 + g) : lane_value(rows8, g);
+        const uint32_t mask = row8 >= 0 ? seen_bits(sk, 32 * kb) : 0u;
+        half8 ones;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ones[i] = (mask >> i) & 1 ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 16 * nb + col), t0 + 8 * g, seen.end);
+          const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(special_marks(v), ones, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[nb][i] += special_sum(n[i]);
+        }
+      }
+    }
   }
 
   // ---- the waves' sums -------------------------------------------------------------------
@@ -279,8 +292,12 @@ void paged_few_kernel(const PagedAttendArgs a) {
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
   }
+  const float f = exact_reference(ref, c);
+  l *= f;
+#pragma unroll
+  for (int nb = 0; nb < 4; ++nb) acc[nb] *= f;
   if (lane < R) {
-    sm[wave][col] = m;
+    sm[wave][col] = ref.m;
     sl[wave][col] = l;
   }
 #pragma unroll
@@ -297,9 +314,9 @@ void paged_few_kernel(const PagedAttendArgs a) {
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    const float f = between(sm[w][r], M, cr);
-    L += f * sl[w][r];
-    o += f * *reinterpret_cast<const f32x4*>(&so[w][r][d]);
+    const float fw = between(sm[w][r], M, cr);
+    L += fw * sl[w][r];
+    o += fw * *reinterpret_cast<const f32x4*>(&so[w][r][d]);
   }
   if (a.plan.few_splits == 1) {
     const int tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));

@@ -15,7 +15,7 @@ __global__ __launch_bounds__(256) void paged_many_merge_kernel(const PagedAttend
   if (r >= t.n * a.G) return;
   const float* part = a.many_part + (((int64_t)index * a.pages.Hkv + kvh) * S * R + in) * kPartial;
   const int64_t next = (int64_t)R * kPartial;
-  float M = -INFINITY;
+  float M = kNoReference;
   for (int s = 0; s < S; ++s) M = fmaxf(M, part[s * next + kDim]);
   float L = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};

@@ -7,8 +7,8 @@
 // Scores S^T = K Q^T by v_mfma_f32_32x32x16_f16 (codes as fp16 weights, the INT8 queries as fp16
 // integers: exact sums), the rows of K in such an order that a lane ends up with the scores of
 // one query and 8 consecutive keys of every 16: the operand of O^T = V^T P^T as they stand. A
-// query's reference, sum and outputs are its two lanes' own. The reference rises only when a weight would
-// leave fp16's range.
+// query's reference, sum and outputs are its two lanes' own. The reference rises only when weights
+// would leave fp16's range.
 #pragma once
 
 #include "paged.hpp"
@@ -72,16 +72,16 @@ struct ManyStage<POT_VALUES_INT4> {
 
 // LOW: the weights' rounding goes into the products too (outputs of 32 bits).
 template <int K, int VF, int NW, bool LOW>
-__global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendArgs a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) void paged_many_kernel(const PagedAttendArgs a) {
   constexpr int R = 32 * NW, kGroups = 8 / NW;  // groups a wave stages
   struct Tile {
     uint4 k[8 * 64];  // chunk d (dimensions 8d ..+7) of key j at 64 d + (j ^ d)
     uint4 v[8 * 64];  // tokens 8g ..+7 of dimension d at 64 g + d
   };
   __shared__ Tile tiles[2];
+  __shared__ uint4 queries[R * 8];  // read again for every tile: the registers are the values'
   __shared__ __attribute__((aligned(16))) float scales[2][64];
   __shared__ __attribute__((aligned(16))) int flags[2][8];  // of a group: 1 not there, 2 holds special values
-  static_assert(sizeof(tiles) >= sizeof(uint4) * R * 8, "the queries pass through the tiles' place");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int S = a.plan.many_splits, Hkv = a.pages.Hkv;
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
 
   // ---- queries: 8 rows of the wave at a time, 8 lanes each ---------------------------------
   const int col = lane & 31, half = lane >> 5;
-  uint4* sq = reinterpret_cast<uint4*>(tiles) + wave * 32 * 8;
+  uint4* sq = queries + wave * 32 * 8;  // the wave's own: chunk d of row r at 8 r + (d ^ r % 8)
   float c = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -109,17 +109,11 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
       load8(a.q, (int64_t)(t.first + tok) * a.q_stride_t + head * a.q_stride_h, lane & 7, a.dtype, x);
     }
     float factor;
-    sq[rw * 8 + (lane & 7)] = quantised_query(x, a.hadamard, lane, &factor);
+    sq[rw * 8 + ((lane ^ rw) & 7)] = quantised_query(x, a.hadamard, lane, &factor);
     // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants row col's
     const float got = __shfl(factor, 8 * (col & 7), 64);
     if ((col >> 3) == i) c = got;
   }
-  __syncthreads();
-  half8 q[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) q[s] = __builtin_bit_cast(half8, sq[col * 8 + 2 * s + half]);
-  __syncthreads();
-
   const int my_row = r0 + 32 * wave + col;
   const bool active = r0 + 32 * wave < rows;
   const int place = t.place + min(my_row, last) / a.G;
@@ -171,7 +165,10 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
       int flag = st_there[i] ? 0 : 1;
       if (part) {  // uniform
         v = mask_tokens(v, t0 + 8 * g, seen.end);
-        if (__any(has_special(v))) flag |= 2;
+        if (__any(has_special(v))) {
+          flag |= 2;
+          v = without_special(v);
+        }
       }
       tiles[buf].v[64 * g + lane] = v;
       if (lane < 8) scales[buf][8 * g + lane] = st[i].scale;
@@ -182,27 +179,24 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
   f32x16 acc[2];
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[0][i] = acc[1][i] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
+  Reference ref;
+  float l = 0.0f;
   // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
   const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
 
-  auto compute = [&](int t0, int buf) {
-    if (!active || none_seen(w_first, w_last, t0, a.window, a.n_sink)) return;
+  auto compute = [&](bool part, int t0, int buf) {
     const Tile& T = tiles[buf];
-    const int4 f0 = *reinterpret_cast<const int4*>(&flags[buf][0]);
-    const int4 f1 = *reinterpret_cast<const int4*>(&flags[buf][4]);
-    const int any = __builtin_amdgcn_readfirstlane(f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w);
-    const bool part = !all_seen(w_first, w_last, t0, a.window, a.n_sink) || (any & 1);
     f32x16 s[2];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = 0.0f;
+    for (int step = 0; step < 4; ++step) {
+      const int d = 2 * step + half;
+      const half8 q = __builtin_bit_cast(half8, sq[8 * col + ((d ^ col) & 7)]);
 #pragma unroll
-      for (int step = 0; step < 4; ++step) {
-        const int d = 2 * step + half;
+      for (int kb = 0; kb < 2; ++kb) {
         const half8 kv = __builtin_bit_cast(half8, T.k[64 * d + ((32 * kb + krow) ^ d)]);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q[step], s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q, s[kb], 0, 0, 0);
       }
     }
 #pragma unroll
@@ -215,72 +209,65 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[kb][8 * u + i] *= sv[i];
       }
-    if (part) {
+    if (part) {  // uniform
+      const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const bool there = !(flags[buf][4 * kb + 2 * u + half] & 1);
+          const uint32_t mask = flags[buf][4 * kb + 2 * u + half] & 1 ? 0u : seen_bits(sk, 32 * kb + 16 * u);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int key = t0 + 32 * kb + 16 * u + 8 * half + i;
-            if (!(there && key < seen.end && sees(place, key, a.window, a.n_sink))) s[kb][8 * u + i] = -INFINITY;
-          }
+          for (int i = 0; i < 8; ++i) s[kb][8 * u + i] = if_seen(s[kb][8 * u + i], mask, i);
         }
     }
-    float top = s[0][0];
+    float top = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
-    for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+    for (int i = 2; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
-    const bool rises = top > m && (m == -INFINITY || (top - m) * c > kMostRise);
-    if (__any(rises)) {
-      const float to = rises ? top : m, f = between(m, to, c);
+    if (must_rise(ref, top, c)) {
+      const float f = raise(ref, top, c);
       acc[0] *= f;
       acc[1] *= f;
       l *= f;
-      m = to;
     }
-    uint32_t hi[16], lo[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int kb = i >> 3, e = 2 * (i & 7);
-      float p0 = paged_weight(s[kb][e], m, c), p1 = paged_weight(s[kb][e + 1], m, c);
-      if (part) {
-        p0 = s[kb][e] == -INFINITY ? 0.0f : p0;
-        p1 = s[kb][e + 1] == -INFINITY ? 0.0f : p1;
-      }
-      l += p0;
-      l += p1;
-      hi[i] = pack_half(p0, p1);
-      if constexpr (LOW) lo[i] = low_part(p0, p1, hi[i]);
+    if (ref.far) {  // uniform
+      s[0] -= ref.m;
+      s[1] -= ref.m;
     }
+    const float shift = weight_shift(ref);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {  // 16 keys at a time
-      const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[4 * b], hi[4 * b + 1], hi[4 * b + 2], hi[4 * b + 3]));
+      const int kb = b >> 1, e0 = 8 * (b & 1);
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = weight_of(s[kb][e0 + 2 * i], c, shift), p1 = weight_of(s[kb][e0 + 2 * i + 1], c, shift);
+        l += p0;
+        l += p1;
+        hi[i] = pack_half(p0, p1);
+        if constexpr (LOW) lo[i] = low_part(p0, p1, hi[i]);
+      }
+      const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb) {
-        half8 v = __builtin_bit_cast(half8, T.v[64 * (2 * b + half) + 32 * nb + col]);
-        if (part && (any & 2)) {  // uniform
-          half8 marks, ones;
-          split_special(v, &v, &marks);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            ones[i] = s[b >> 1][8 * (b & 1) + i] == -INFINITY ? (_Float16)0.0f : (_Float16)1.0f;
-          f32x16 n;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
-          n = __builtin_amdgcn_mfma_f32_32x32x16_f16(marks, ones, n, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[nb][i] += special_sum(n[i]);
-        }
+        const half8 v = __builtin_bit_cast(half8, T.v[64 * (2 * b + half) + 32 * nb + col]);
         acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[nb], 0, 0, 0);
         if constexpr (LOW) {
-          const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[4 * b], lo[4 * b + 1], lo[4 * b + 2], lo[4 * b + 3]));
+          const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
           acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[nb], 0, 0, 0);
         }
       }
     }
+  };
+  bool special = false;  // a tile in part held special values (paged.hpp); uniform
+  auto tile = [&](int t0, int buf) {
+    if (!active || none_seen(w_first, w_last, t0, a.window, a.n_sink)) return;
+    const int4 f0 = *reinterpret_cast<const int4*>(&flags[buf][0]);
+    const int4 f1 = *reinterpret_cast<const int4*>(&flags[buf][4]);
+    const int any = __builtin_amdgcn_readfirstlane(f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w);
+    compute(!all_seen(w_first, w_last, t0, a.window, a.n_sink) || (any & 1), t0, buf);
+    special |= (any & 2) != 0;
   };
 
   int buf = 0;
@@ -293,9 +280,38 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
   for (int j = run.first; j < run.end; ++j) {
     __syncthreads();
     if (j + 1 < run.end) load(j + 1);
-    compute(tile_start(seen, j), buf);
+    tile(tile_start(seen, j), buf);
     if (j + 1 < run.end) stage(j + 1, buf ^ 1);
     buf ^= 1;
+  }
+
+  if (special) {
+#pragma nounroll
+    for (int j = run.first; j < run.end; ++j) {
+      const int t0 = tile_start(seen, j);
+      if (all_seen(wg_first, wg_last, t0, a.window, a.n_sink)) continue;
+      const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
+#pragma nounroll
+      for (int b = 0; b < 4; ++b) {
+        const int g = 2 * b + half;
+        const int row8 = t0 + 8 * g < seen.end ? group_row8(a.pages, table, kvh, t0 / 8 + g) : -1;
+        const uint32_t mask = row8 >= 0 ? seen_bits(sk, 16 * b) : 0u;
+        half8 ones;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ones[i] = (mask >> i) & 1 ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 32 * nb + col), t0 + 8 * g, seen.end);
+          f32x16 n;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+          n = __builtin_amdgcn_mfma_f32_32x32x16_f16(special_marks(v), ones, n, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[nb][i] += special_sum(n[i]);
+        }
+      }
+    }
   }
 
   const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -313,6 +329,10 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
                    acc[nb][4 * i + 2] * inv, acc[nb][4 * i + 3] * inv);
     return;
   }
+  const float f = exact_reference(ref, c);
+  l *= f;
+  acc[0] *= f;
+  acc[1] *= f;
   float* part = a.many_part + ((((int64_t)index * Hkv + kvh) * S + split) * R + (my_row - r0)) * kPartial;
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb)
@@ -320,7 +340,7 @@ __global__ __launch_bounds__(64 * NW) void paged_many_kernel(const PagedAttendAr
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<f32x4*>(part + 32 * nb + 8 * i + 4 * half) =
           f32x4{acc[nb][4 * i], acc[nb][4 * i + 1], acc[nb][4 * i + 2], acc[nb][4 * i + 3]};
-  if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{m, l, c, 0.0f};
+  if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{ref.m, l, c, 0.0f};
 }
 
 template <int K, int VF, int NW>
