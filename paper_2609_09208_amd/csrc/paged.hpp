@@ -14,6 +14,17 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+// Loads past the caches, of what a call reads once.
+__device__ __forceinline__ uint4 stream16(const void* p) {
+  const u32x4v v = __builtin_nontemporal_load(static_cast<const u32x4v*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint2 stream8(const void* p) {
+  const u32x2v v = __builtin_nontemporal_load(static_cast<const u32x2v*>(p));
+  return make_uint2(v.x, v.y);
+}
+
 // A group's rows of the pool are counted by groups: row8 = row / 8, below 2^31.
 // First cache row / 8 of group `group` of a sequence for a kv head: group `in` of its page;
 // -1 where the table has no such page. table: the sequence's entries.
@@ -287,6 +298,56 @@ __device__ __forceinline__ float raise(Reference& r, float top, float c) {
 __device__ __forceinline__ float exact_reference(const Reference& r, float c) {
   return r.far || r.m == kNoReference
              ? 1.0f : __builtin_amdgcn_exp2f(-__builtin_fmaf(r.m, c, r.b - kWeightShift));
+}
+
+// A row's partials of S key ranges (`next` floats apart) as one by a wave, of which lane l takes
+// dimensions 4 (l % 16) ..+3 of ranges l / 16, 4 + l / 16 ..; the quotients in every lane.
+struct Merged {
+  float o[4];
+};
+__device__ __forceinline__ float over_rows(float v) {  // sum over the wave's 16-lane rows
+  const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r16[0]) + __uint_as_float(r16[1]);
+  const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
+}
+__device__ __forceinline__ Merged merge_parts(const float* part, int next, int S, int lane) {
+  const int grp = lane >> 4, d = 4 * (lane & 15);
+  float M = kNoReference, c = 0.0f, L = 0.0f;
+  f32x4 O = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = 0; s0 < S; s0 += 16) {
+    f32x4 w[4], o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* p = part + (int64_t)min(s0 + 4 * i + grp, S - 1) * next;
+      w[i] = *reinterpret_cast<const f32x4*>(p + kDim);
+      o[i] = *reinterpret_cast<const f32x4*>(p + d);
+    }
+    c = w[0][2];
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, w[i][0]);
+    const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+    const float f0 = between(M, top, c);
+    L *= f0;
+    O *= f0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = s0 + 4 * i + grp < S ? between(w[i][0], top, c) : 0.0f;
+      L += f * w[i][1];
+      O += f * o[i];
+    }
+    M = top;
+  }
+  L = over_rows(L);
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  Merged g;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) g.o[i] = over_rows(O[i]) * inv;
+  return g;
 }
 
 }  // namespace potattn

@@ -97,13 +97,13 @@ void paged_few_kernel(const PagedAttendArgs a) {
       ks[kb][1] = sp[1];
       if constexpr (VF == POT_VALUES_INT4) {
         const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
-        vr.f[kb] = *reinterpret_cast<const uint4*>(rec + 16 * col);
+        vr.f[kb] = stream16(rec + 16 * col);
         vr.s[kb] = *reinterpret_cast<const uint4*>(rec + kI4Steps);
         vr.z[kb] = *reinterpret_cast<const uint4*>(rec + kI4Minima);
       } else {
         const uint8_t* v = a.pages.values + row8 * (16 * kDim) + 16 * col;
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb) vr.f[kb][nb] = *reinterpret_cast<const uint4*>(v + 256 * nb);
+        for (int nb = 0; nb < 4; ++nb) vr.f[kb][nb] = stream16(v + 256 * nb);
       }
     }
   };
