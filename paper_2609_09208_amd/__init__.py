@@ -525,40 +525,46 @@ def make_pages(codes_se, codes_m, key_scale, values, table) -> pot_pages:
     pages = pot_pages(_ptr(codes_se), _ptr(codes_m), _ptr(key_scale), _ptr(values), _ptr(table),
                       POT_VALUES_INT4 if int4 else POT_VALUES_FP16, n_pages, Hkv, page_size, table.shape[1])
     pages.tensors = (codes_se, codes_m, key_scale, values, table)
+    pages.calls = (table.shape[0], device, 0 if codes_m is None else k, Hkv)  # what every call checks
     return pages
 
 
-def _sequences(pages, cu_new, seq_lens, device) -> int:
-    """B of a call over pages, whose sequences' bounds and lengths the kernels read as int32."""
-    table = pages.tensors[4]
-    B = table.shape[0]
-    if (cu_new.dtype is not torch.int32 or seq_lens.dtype is not torch.int32 or cu_new.numel() != B + 1
-            or seq_lens.numel() != B or not cu_new.is_contiguous() or not seq_lens.is_contiguous()
-            or cu_new.get_device() != device or seq_lens.get_device() != device
-            or table.get_device() != device):
-        _mismatch("cu_new is dense int32 [B + 1], seq_lens [B], on the rows' GPU, as are the pages")
-    return B
-
-
-def _key_format(fmt, pages) -> None:
-    codes_m = pages.tensors[1]
-    if fmt.mant_bits != (0 if codes_m is None else codes_m.shape[-1] // 8):
+def _sequences(fmt, pages, cu_new, seq_lens, device):
+    """B and Hkv of a call over pages, and the addresses of the sequences' bounds and lengths, which the kernels
+    read as int32."""
+    B, on, k, Hkv = pages.calls
+    if fmt.mant_bits != k:
         _mismatch("the pages hold keys of another mant_bits")
+    i32 = torch.int32
+    if (cu_new.dtype is not i32 or seq_lens.dtype is not i32 or cu_new.numel() != B + 1 or seq_lens.numel() != B
+            or not cu_new.is_contiguous() or not seq_lens.is_contiguous() or cu_new.get_device() != device
+            or seq_lens.get_device() != device or on != device):
+        _mismatch("cu_new is dense int32 [B + 1], seq_lens [B], on the rows' GPU, as are the pages")
+    return B, Hkv, cu_new.data_ptr(), seq_lens.data_ptr()
 
 
-def _packed(x, heads, weight, out, dtype, device, n):
-    """pot_part of packed rows [n, heads, 64] (any strides, elements side by side)."""
-    if (x.dim() != 3 or x.shape[0] != n or x.shape[2] != HEAD_DIM or x.stride(2) != 1 or x.dtype is not dtype
-            or x.get_device() != device or (heads is not None and x.shape[1] != heads)):
+def _packed(x, heads, weight, dtype, device, n, out):
+    """Rows and heads of packed rows [n, heads, 64] (any strides, elements side by side; of n and heads, if
+    given), and their pot_part. The output is dense and of the rows' size."""
+    try:
+        rows, h, d = x.shape
+    except ValueError:  # not three dimensions
+        _mismatch("rows [n, heads, 64] are needed")
+    st, sh, se = x.stride()
+    if (d != HEAD_DIM or se != 1 or x.dtype is not dtype or x.get_device() != device
+            or (n is not None and rows != n) or (heads is not None and h != heads)):
         _mismatch("rows [n, heads, 64] of one type with dense elements on one GPU are needed")
-    if weight is not None and (weight.numel() != HEAD_DIM or not weight.is_contiguous()
-                               or weight.get_device() != device):
-        _mismatch("weights are [64] and dense, on the rows' GPU")
-    if out is not None and (tuple(out.shape) != tuple(x.shape) or not out.is_contiguous()
-                            or out.get_device() != device):
-        _mismatch("a dense output [n, heads, 64] on the rows' GPU is needed")
-    return _pack_part(x.data_ptr(), 0, x.stride(0), x.stride(1), 0 if weight is None else weight.data_ptr(),
-                      0 if out is None else out.data_ptr())
+    o = w = 0
+    if out is not None:
+        if out.numel() != rows * h * HEAD_DIM or not out.is_contiguous() or out.get_device() != device:
+            _mismatch("a dense output [n, Hq, 64] on the rows' GPU is needed")
+        o = out.data_ptr()
+    if weight is not None:
+        if (weight.numel() != HEAD_DIM or not weight.is_contiguous()
+                or weight.get_device() != device):
+            _mismatch("weights are [64] and dense, on the rows' GPU")
+        w = weight.data_ptr()
+    return rows, h, _pack_part(x.data_ptr(), 0, st, sh, w, o)
 
 
 def pot_paged_append(fmt: pot_format, rope: pot_rope, q, k, v, q_weight, k_weight, eps: float, positions,
@@ -567,37 +573,40 @@ def pot_paged_append(fmt: pot_format, rope: pot_rope, q, k, v, q_weight, k_weigh
     all sequences side by side, sequence b's being rows cu_new[b] .. cu_new[b + 1] - 1 and the last of its
     seq_lens[b]; k and v go into the pages, q to q_out [n, Hq, 64] (dense). positions int64 [n_axes, n] or
     None (places in the sequence), inv_freq float64 [rot_dim / 2], weights [64] of one type or None."""
-    dtype, device, n = k.dtype, k.get_device(), k.shape[0]
+    dtype, device, types = k.dtype, k.get_device(), _DTYPES
     if device < 0:
         _mismatch("tensors on the GPU are needed")
-    B = _sequences(pages, cu_new, seq_lens, device)
-    _key_format(fmt, pages)
-    Hq, parts = 0, _NO_PART
-    if q is not None:
+    B, Hkv, cu, lens = _sequences(fmt, pages, cu_new, seq_lens, device)
+    itype = types.get(dtype)
+    n, _, part_k = _packed(k, Hkv, k_weight, dtype, device, None, None)
+    part_v = _packed(v, Hkv, None, dtype, device, n, None)[2]
+    if q is None:
+        Hq, part_q, qtype, w = 0, _NO_PART, POT_FP32, k_weight
+    else:
         if q_out is None:
             _mismatch("q needs an output")
-        Hq, parts = q.shape[1], _packed(q, None, q_weight, q_out, dtype, device, n)
-    parts += _packed(k, pages.Hkv, k_weight, None, dtype, device, n)
-    parts += _packed(v, pages.Hkv, None, None, dtype, device, n)
-    if q is None:
-        q_weight = None
-    w = q_weight if q_weight is not None else k_weight
+        _, Hq, part_q = _packed(q, None, q_weight, dtype, device, n, q_out)
+        qtype, w = types.get(q_out.dtype), k_weight if q_weight is None else q_weight
+    wtype = itype
+    if w is not None and w.dtype is not dtype:
+        wtype = types.get(w.dtype)
     if k_weight is not None and k_weight.dtype is not w.dtype:
         _mismatch("weights are of one type")
-    if positions is not None and (positions.dtype is not torch.int64 or not positions.is_contiguous()
-                                  or positions.numel() != rope.n_axes * n or positions.get_device() != device):
-        _mismatch("positions are dense int64 [n_axes, n] on the rows' GPU")
-    if inv_freq is not None and (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
-                                 or inv_freq.numel() < rope.rot_dim // 2 or inv_freq.get_device() != device):
-        _mismatch("inv_freq is dense float64 [rot_dim / 2] on the rows' GPU")
-    itype, wtype = _DTYPES.get(dtype), _DTYPES.get(dtype if w is None else w.dtype)
-    qtype = POT_FP32 if q is None else _DTYPES.get(q_out.dtype)
+    at = turns = None
+    if positions is not None:
+        if (positions.dtype is not torch.int64 or not positions.is_contiguous()
+                or positions.numel() != rope.n_axes * n or positions.get_device() != device):
+            _mismatch("positions are dense int64 [n_axes, n] on the rows' GPU")
+        at = positions.data_ptr()
+    if inv_freq is not None:
+        if (inv_freq.dtype is not torch.float64 or not inv_freq.is_contiguous()
+                or inv_freq.numel() < rope.rot_dim // 2 or inv_freq.get_device() != device):
+            _mismatch("inv_freq is dense float64 [rot_dim / 2] on the rows' GPU")
+        turns = inv_freq.data_ptr()
     if itype is None or wtype is None or qtype is None:
         _mismatch("types are float16, bfloat16 or float32")
-    status = _lib.pot_paged_append(
-        fmt, rope, itype, parts, wtype, eps, None if positions is None else positions.data_ptr(),
-        None if inv_freq is None else inv_freq.data_ptr(), pages, cu_new.data_ptr(), seq_lens.data_ptr(), B, n,
-        Hq, qtype, _stream(stream, device))
+    status = _lib.pot_paged_append(fmt, rope, itype, part_q + part_k + part_v, wtype, eps, at, turns, pages, cu, lens, B, n, Hq, qtype,
+                                   _stream(stream, device))
     if status:
         _check(status)
 
@@ -613,29 +622,32 @@ def pot_paged_attention(fmt: pot_format, q, pages: pot_pages, cu_new, seq_lens, 
     keys and values are in the pages), to out [n, Hq, 64] (dense). A query sees its sequence up to itself, with
     a window the last `window` tokens of that and the first n_sink."""
     try:
-        n, Hq, d = q.shape
-        st, sh, se = q.stride()
-    except ValueError:
+        n, Hq, d = shape = q.shape
+    except ValueError:  # not three dimensions
         _mismatch("queries [n, Hq, 64] are needed")
+    st, sh, se = q.stride()
     device = q.get_device()
     if device < 0:
         _mismatch("tensors on the GPU are needed")
-    if (d != HEAD_DIM or se != 1 or tuple(out.shape) != (n, Hq, d) or not out.is_contiguous()
+    if (d != HEAD_DIM or se != 1 or out.shape != shape or not out.is_contiguous()
             or out.get_device() != device):
         _mismatch("queries and a dense output [n, Hq, 64] on one GPU are needed")
-    B = _sequences(pages, cu_new, seq_lens, device)
-    _key_format(fmt, pages)
+    B, _, cu, lens = _sequences(fmt, pages, cu_new, seq_lens, device)
     itype, otype = _DTYPES.get(q.dtype), _DTYPES.get(out.dtype)
     if itype is None or otype is None:
         _mismatch("types are float16, bfloat16 or float32")
     heads, hp = _heads(kv_head_of_q)
     if heads.size != Hq:
         _mismatch("kv_head_of_q has Hq entries")
-    if workspace is not None and ws_bytes is None:
-        ws_bytes = workspace.numel() * workspace.element_size()
-    status = _lib.pot_paged_attention(
-        fmt, itype, q.data_ptr(), st, sh, pages, cu_new.data_ptr(), seq_lens.data_ptr(), hp, B, n, Hq, max_new,
-        max_len, window, n_sink, otype, out.data_ptr(), _ptr(workspace), ws_bytes or 0, _stream(stream, device))
+    if workspace is None:
+        ws = ws_bytes = 0
+    else:
+        ws = _ptr(workspace)
+        if ws_bytes is None:
+            ws_bytes = workspace.numel() * workspace.element_size()
+    status = _lib.pot_paged_attention(fmt, itype, q.data_ptr(), st, sh, pages, cu, lens, hp, B, n, Hq, max_new,
+                                      max_len, window, n_sink, otype, out.data_ptr(), ws, ws_bytes,
+                                      _stream(stream, device))
     if status:
         _check(status)
 

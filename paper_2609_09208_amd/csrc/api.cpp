@@ -635,11 +635,11 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
     p.few_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 * few_per_cu / units, most, 64}));
   }
   if (many) {
-    p.many_waves = rows > 128 ? 8 : 4;
-    const int64_t R = 32 * p.many_waves, full = ((int64_t)n * G + R - 1) / R;
+    p.many_rows = rows > 128 ? 256 : 128;
+    const int64_t R = p.many_rows, full = ((int64_t)n * G + R - 1) / R;
     p.many_tiles = (int64_t)n * G / R + std::min(B, n);
     const int64_t most = (tiles + 7) / 8;
-    p.many_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 * 8 / p.many_waves / (full * Hkv), most, 32}));
+    p.many_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / (full * Hkv), most, 32}));
   }
   return p;
 }
@@ -653,7 +653,7 @@ PagedLayout paged_layout(const PagedPlan& p, int B, int Hkv) {
     w.many = align_up((size_t)B * Hkv * p.few_splits * kFewRows * kPartial * 4, 256);
   w.total = w.many;
   if (p.many_splits > 1)
-    w.total += align_up((size_t)p.many_tiles * Hkv * p.many_splits * 32 * p.many_waves * kPartial * 4, 256);
+    w.total += align_up((size_t)p.many_tiles * Hkv * p.many_splits * p.many_rows * kPartial * 4, 256);
   return w;
 }
 

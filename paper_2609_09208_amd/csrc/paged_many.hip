@@ -6,7 +6,7 @@ namespace potattn {
 
 // The same merge for the rows of a row tile, a wave per row, four rows a workgroup.
 __global__ __launch_bounds__(256) void paged_many_merge_kernel(const PagedAttendArgs a) {
-  const int R = 32 * a.plan.many_waves, S = a.plan.many_splits;
+  const int R = a.plan.many_rows, S = a.plan.many_splits;
   const int piece = blockIdx.x % (R / 4), kvh = blockIdx.y, index = blockIdx.x / (R / 4);
   const RowTile at = find_tile(a, index, R);
   if (at.b < 0) return;
@@ -22,26 +22,26 @@ __global__ __launch_bounds__(256) void paged_many_merge_kernel(const PagedAttend
              g.o[2], g.o[3]);
 }
 
-template <int VF, int NW>
+template <int VF, int RB>
 static hipError_t launch_k(const PagedAttendArgs& a, hipStream_t stream) {
   switch (a.mant_bits) {
-    case 0: return launch_many<0, VF, NW>(a, stream);
-    case 1: return launch_many<1, VF, NW>(a, stream);
-    case 2: return launch_many<2, VF, NW>(a, stream);
-    case 3: return launch_many<3, VF, NW>(a, stream);
-    default: return launch_many<4, VF, NW>(a, stream);
+    case 0: return launch_many<0, VF, RB>(a, stream);
+    case 1: return launch_many<1, VF, RB>(a, stream);
+    case 2: return launch_many<2, VF, RB>(a, stream);
+    case 3: return launch_many<3, VF, RB>(a, stream);
+    default: return launch_many<4, VF, RB>(a, stream);
   }
 }
 
 hipError_t launch_paged_many(const PagedAttendArgs& a, hipStream_t stream) {
-  const hipError_t e = a.plan.many_waves == 8
-                           ? (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 8>(a, stream)
-                                                                : launch_k<POT_VALUES_FP16, 8>(a, stream))
-                           : (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 4>(a, stream)
-                                                                : launch_k<POT_VALUES_FP16, 4>(a, stream));
+  const hipError_t e = a.plan.many_rows == 256
+                           ? (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 2>(a, stream)
+                                                                : launch_k<POT_VALUES_FP16, 2>(a, stream))
+                           : (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 1>(a, stream)
+                                                                : launch_k<POT_VALUES_FP16, 1>(a, stream));
   if (e != hipSuccess || a.plan.many_splits == 1) return e;
   hipLaunchKernelGGL(paged_many_merge_kernel,
-                     dim3((uint32_t)(a.plan.many_tiles * (8 * a.plan.many_waves)), (uint32_t)a.pages.Hkv),
+                     dim3((uint32_t)(a.plan.many_tiles * (a.plan.many_rows / 4)), (uint32_t)a.pages.Hkv),
                      dim3(256), 0, stream, a);
   return hipGetLastError();
 }

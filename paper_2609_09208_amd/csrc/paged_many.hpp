@@ -1,8 +1,8 @@
 // Attention over a paged cache for sequences with many rows (new tokens x query heads of a kv
-// head): chunks of prompts. A workgroup takes a tile of 32 NW rows of one sequence and kv head,
-// 32 rows a wave, and goes through the 64-key tiles that some of its rows see; the keys' codes
-// and the values become fp16 operands in LDS once for all its waves, the next tile's loads under
-// way meanwhile.
+// head): chunks of prompts. A workgroup of four waves takes a tile of 128 RB rows of one sequence
+// and kv head, RB blocks of 32 rows a wave, and goes through the 64-key tiles that some of its rows
+// see; the keys' codes and the values become fp16 operands in LDS once for all its waves, the next
+// tile's loads under way meanwhile, and a wave reads them once for its RB blocks.
 //
 // Scores S^T = K Q^T by v_mfma_f32_32x32x16_f16 (codes as fp16 weights, the INT8 queries as fp16
 // integers: exact sums), the rows of K in such an order that a lane ends up with the scores of
@@ -70,18 +70,21 @@ struct ManyStage<POT_VALUES_INT4> {
   uint4 s, z;
 };
 
-// LOW: the weights' rounding goes into the products too (outputs of 32 bits).
-template <int K, int VF, int NW, bool LOW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) void paged_many_kernel(const PagedAttendArgs a) {
-  constexpr int R = 32 * NW, kGroups = 8 / NW;  // groups a wave stages
+constexpr int kManyWaves = 4;
+
+// RB: row blocks a wave. LOW: the weights' rounding goes into the products too (outputs of 32 bits).
+template <int K, int VF, int RB, bool LOW>
+__global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(RB == 2 ? 2 : 3)))
+void paged_many_kernel(const PagedAttendArgs a) {
+  constexpr int NW = kManyWaves, R = 32 * RB * NW, kGroups = 8 / NW;  // groups a wave stages
   struct Tile {
     uint4 k[8 * 64];  // chunk d (dimensions 8d ..+7) of key j at 64 d + (j ^ d)
     uint4 v[8 * 64];  // tokens 8g ..+7 of dimension d at 64 g + d
   };
   __shared__ Tile tiles[2];
-  __shared__ uint4 queries[R * 8];  // read again for every tile: the registers are the values'
   __shared__ __attribute__((aligned(16))) float scales[2][64];
   __shared__ __attribute__((aligned(16))) int flags[2][8];  // of a group: 1 not there, 2 holds special values
+  static_assert(sizeof(tiles) >= sizeof(uint4) * R * 8, "the queries pass through the tiles' place");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int S = a.plan.many_splits, Hkv = a.pages.Hkv;
@@ -91,65 +94,44 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
   const NewTokens t = sequence_tokens(a.packed, at.b, a.max_new, a.max_len);
   const int rows = t.n * a.G, r0 = at.tile * R;
   const int last = min(r0 + R, rows) - 1;
-  const SeenTiles seen = seen_tiles(t.place + r0 / a.G, t.place + last / a.G, t.len, a.window, a.n_sink);
-  const TileRun run = split_tiles(seen.tiles, split, S);
   const int wg_first = t.place + r0 / a.G, wg_last = t.place + last / a.G;
+  const SeenTiles seen = seen_tiles(wg_first, wg_last, t.len, a.window, a.n_sink);
+  const TileRun run = split_tiles(seen.tiles, split, S);
   const int32_t* table = a.pages.table + (int64_t)at.b * a.pages.table_len;
-
-  // ---- queries: 8 rows of the wave at a time, 8 lanes each ---------------------------------
   const int col = lane & 31, half = lane >> 5;
-  uint4* sq = queries + wave * 32 * 8;  // the wave's own: chunk d of row r at 8 r + (d ^ r % 8)
-  float c = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int rw = 8 * i + (lane >> 3), r = r0 + 32 * wave + rw;
-    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (r < rows) {
-      const int tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));
-      load8(a.q, (int64_t)(t.first + tok) * a.q_stride_t + head * a.q_stride_h, lane & 7, a.dtype, x);
-    }
-    float factor;
-    sq[rw * 8 + ((lane ^ rw) & 7)] = quantised_query(x, a.hadamard, lane, &factor);
-    // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants row col's
-    const float got = __shfl(factor, 8 * (col & 7), 64);
-    if ((col >> 3) == i) c = got;
-  }
-  const int my_row = r0 + 32 * wave + col;
-  const bool active = r0 + 32 * wave < rows;
-  const int place = t.place + min(my_row, last) / a.G;
-  const int w_first = t.place + min(r0 + 32 * wave, last) / a.G;
-  const int w_last = t.place + min(r0 + 32 * wave + 31, last) / a.G;
+  const int wr0 = r0 + 32 * RB * wave;  // the wave's first row
 
   // ---- staging: wave w has groups w, w + NW .. of the tile --------------------------------
   ManyStage<VF> st[kGroups];
-  bool st_there[kGroups];
-  auto load = [&](int j) {
-    const int g0 = tile_start(seen, j) / 8;
+  int st_row[kGroups], next_row[kGroups];  // first cache row / 8, -1: not there
+  auto find_rows = [&](int j) {
+    const int g0 = tile_start(seen, min(j, run.end - 1)) / 8;
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
       const int g = g0 + wave + NW * i;
-      const int row8 = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
-      st_there[i] = row8 >= 0;
-      st[i] = ManyStage<VF>{};
-      if (row8 >= 0) {
-        const int64_t row = (int64_t)row8 * 8 + (lane >> 3);
-        st[i].code = *reinterpret_cast<const uint32_t*>(a.pages.codes_se + row * 32 + 4 * (lane & 7));
+      next_row[i] = g * 8 < seen.end ? group_row8(a.pages, table, kvh, g) : -1;
+    }
+  };
+  auto load = [&]() {  // the groups of next_row; those not there read row 0
 #pragma unroll
-        for (int p = 0; p < K; ++p) st[i].plane[p] = a.pages.codes_m[row * 8 * K + 8 * p + (lane & 7)];
-        if (lane < 8) st[i].scale = a.pages.key_scale[(int64_t)row8 * 8 + lane];
-        if constexpr (VF == POT_VALUES_INT4) {
-          const uint8_t* rec = a.pages.values + (int64_t)row8 * kI4GroupBytes;
-          st[i].n = *reinterpret_cast<const uint2*>(rec + 16 * (lane & 15) + 8 * (lane >> 5));
-          st[i].s = *reinterpret_cast<const uint4*>(rec + kI4Steps);
-          st[i].z = *reinterpret_cast<const uint4*>(rec + kI4Minima);
-        } else {
-          st[i].v = *reinterpret_cast<const uint4*>(a.pages.values + (int64_t)row8 * (16 * kDim) + 16 * lane);
-        }
+    for (int i = 0; i < kGroups; ++i) {
+      st_row[i] = next_row[i];
+      const int64_t row8 = max(next_row[i], 0), row = row8 * 8 + (lane >> 3);
+      st[i].code = *reinterpret_cast<const uint32_t*>(a.pages.codes_se + row * 32 + 4 * (lane & 7));
+#pragma unroll
+      for (int p = 0; p < K; ++p) st[i].plane[p] = a.pages.codes_m[row * 8 * K + 8 * p + (lane & 7)];
+      st[i].scale = a.pages.key_scale[row8 * 8 + (lane & 7)];
+      if constexpr (VF == POT_VALUES_INT4) {
+        const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
+        st[i].n = *reinterpret_cast<const uint2*>(rec + 16 * (lane & 15) + 8 * (lane >> 5));
+        st[i].s = *reinterpret_cast<const uint4*>(rec + kI4Steps);
+        st[i].z = *reinterpret_cast<const uint4*>(rec + kI4Minima);
+      } else {
+        st[i].v = *reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim) + 16 * lane);
       }
     }
   };
-  auto stage = [&](int j, int buf) {
-    const int t0 = tile_start(seen, j);
+  auto stage = [&](int t0, int buf) {
     const bool part = !all_seen(wg_first, wg_last, t0, a.window, a.n_sink);
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
@@ -162,9 +144,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
       } else {
         v = st[i].v;
       }
-      int flag = st_there[i] ? 0 : 1;
-      if (part) {  // uniform
-        v = mask_tokens(v, t0 + 8 * g, seen.end);
+      int flag = st_row[i] >= 0 ? 0 : 1;
+      if (part || flag) {  // uniform
+        v = mask_tokens(v, t0 + 8 * g, flag ? 0 : seen.end);
         if (__any(has_special(v))) {
           flag |= 2;
           v = without_special(v);
@@ -175,30 +157,73 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
       if (lane == 0) flags[buf][g] = flag;
     }
   };
+  if (run.first < run.end) {
+    find_rows(run.first);
+    load();
+    find_rows(run.first + 1);
+  }
 
-  f32x16 acc[2];
+  // ---- queries: 8 rows of the wave at a time, 8 lanes each ---------------------------------
+  uint4* sq = reinterpret_cast<uint4*>(tiles) + wave * 32 * RB * 8;  // chunk d of row r at 8 r + (d ^ r % 8)
+  float c[RB];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) acc[0][i] = acc[1][i] = 0.0f;
-  Reference ref;
-  float l = 0.0f;
+  for (int i = 0; i < 4 * RB; ++i) {
+    const int rw = 8 * i + (lane >> 3), r = wr0 + rw;
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (r < rows) {
+      const int tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));
+      load8(a.q, (int64_t)(t.first + tok) * a.q_stride_t + head * a.q_stride_h, lane & 7, a.dtype, x);
+    }
+    float factor;
+    sq[rw * 8 + ((lane ^ rw) & 7)] = quantised_query(x, a.hadamard, lane, &factor);
+    // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants that of rows col, 32 + col ..
+    const float got = __shfl(factor, 8 * (col & 7), 64);
+    if ((col >> 3) == (i & 3)) c[i >> 2] = got;
+  }
+  __syncthreads();
+  half8 q[RB][4];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      q[rb][s] = __builtin_bit_cast(half8, sq[8 * (32 * rb + col) + ((2 * s + half) ^ (col & 7))]);
+  __syncthreads();
+
+  const bool active = wr0 < rows;
+  const int w_first = t.place + min(wr0, last) / a.G, w_last = t.place + min(wr0 + 32 * RB - 1, last) / a.G;
+  int place[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) place[rb] = t.place + min(wr0 + 32 * rb + col, last) / a.G;
+
+  f32x16 acc[RB][2];
+  Reference ref[RB];
+  float l[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[rb][0][i] = acc[rb][1][i] = 0.0f;
+    l[rb] = 0.0f;
+  }
   // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
   const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
 
   auto compute = [&](bool part, int t0, int buf) {
     const Tile& T = tiles[buf];
-    f32x16 s[2];
+    f32x16 s[RB][2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
+    for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int step = 0; step < 4; ++step) {
-      const int d = 2 * step + half;
-      const half8 q = __builtin_bit_cast(half8, sq[8 * col + ((d ^ col) & 7)]);
+      for (int i = 0; i < 16; ++i) s[rb][0][i] = s[rb][1][i] = 0.0f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int step = 0; step < 4; ++step) {
+        const int d = 2 * step + half;
         const half8 kv = __builtin_bit_cast(half8, T.k[64 * d + ((32 * kb + krow) ^ d)]);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q, s[kb], 0, 0, 0);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q[rb][step], s[rb][kb], 0, 0, 0);
       }
-    }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -207,55 +232,84 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
         const float4 a0 = sp[0], a1 = sp[1];
         const float sv[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[kb][8 * u + i] *= sv[i];
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[rb][kb][8 * u + i] *= sv[i];
       }
     if (part) {  // uniform
-      const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int rb = 0; rb < RB; ++rb) {
+        const SeenKeys sk = seen_keys(a, place[rb], seen.end, t0 + 8 * half);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t mask = flags[buf][4 * kb + 2 * u + half] & 1 ? 0u : seen_bits(sk, 32 * kb + 16 * u);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s[kb][8 * u + i] = if_seen(s[kb][8 * u + i], mask, i);
-        }
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t mask = flags[buf][4 * kb + 2 * u + half] & 1 ? 0u : seen_bits(sk, 32 * kb + 16 * u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[rb][kb][8 * u + i] = if_seen(s[rb][kb][8 * u + i], mask, i);
+          }
+      }
     }
-    float top = fmaxf(s[0][0], s[0][1]);
+    float top[RB];
+    bool rises = false;
 #pragma unroll
-    for (int i = 2; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-    top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
-    if (must_rise(ref, top, c)) {
-      const float f = raise(ref, top, c);
-      acc[0] *= f;
-      acc[1] *= f;
-      l *= f;
+    for (int rb = 0; rb < RB; ++rb) {
+      top[rb] = fmaxf(s[rb][0][0], s[rb][0][1]);
+#pragma unroll
+      for (int i = 2; i < 32; ++i) top[rb] = fmaxf(top[rb], s[rb][i >> 4][i & 15]);
+      const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[rb]), __float_as_uint(top[rb]), false, false);
+      top[rb] = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+      rises |= must_rise(ref[rb], top[rb], c[rb]);
     }
-    if (ref.far) {  // uniform
-      s[0] -= ref.m;
-      s[1] -= ref.m;
+    bool far = false;
+    if (rises) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float f = raise(ref[rb], top[rb], c[rb]);
+        acc[rb][0] *= f;
+        acc[rb][1] *= f;
+        l[rb] *= f;
+      }
     }
-    const float shift = weight_shift(ref);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) far |= ref[rb].far;
+    if (far) {  // uniform
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float off = ref[rb].far ? ref[rb].m : 0.0f;
+        s[rb][0] -= off;
+        s[rb][1] -= off;
+      }
+    }
+    float shift[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) shift[rb] = weight_shift(ref[rb]);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {  // 16 keys at a time
       const int kb = b >> 1, e0 = 8 * (b & 1);
-      uint32_t hi[4], lo[4];
+      uint32_t hi[RB][4], lo[RB][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p0 = weight_of(s[kb][e0 + 2 * i], c, shift), p1 = weight_of(s[kb][e0 + 2 * i + 1], c, shift);
-        l += p0;
-        l += p1;
-        hi[i] = pack_half(p0, p1);
-        if constexpr (LOW) lo[i] = low_part(p0, p1, hi[i]);
-      }
-      const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = weight_of(s[rb][kb][e0 + 2 * i], c[rb], shift[rb]);
+          const float p1 = weight_of(s[rb][kb][e0 + 2 * i + 1], c[rb], shift[rb]);
+          l[rb] += p0;
+          l[rb] += p1;
+          hi[rb][i] = pack_half(p0, p1);
+          if constexpr (LOW) lo[rb][i] = low_part(p0, p1, hi[rb][i]);
+        }
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb) {
         const half8 v = __builtin_bit_cast(half8, T.v[64 * (2 * b + half) + 32 * nb + col]);
-        acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[nb], 0, 0, 0);
-        if constexpr (LOW) {
-          const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-          acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[nb], 0, 0, 0);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[rb][0], hi[rb][1], hi[rb][2], hi[rb][3]));
+          acc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[rb][nb], 0, 0, 0);
+          if constexpr (LOW) {
+            const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[rb][0], lo[rb][1], lo[rb][2], lo[rb][3]));
+            acc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[rb][nb], 0, 0, 0);
+          }
         }
       }
     }
@@ -271,17 +325,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
   };
 
   int buf = 0;
-  if (run.first < run.end) {
-    load(run.first);
-    stage(run.first, 0);
-  }
+  if (run.first < run.end) stage(tile_start(seen, run.first), 0);
   // a barrier a tile: it stands between the staging of a place and its use, and between its use
   // and its next staging, which comes a tile later
+#pragma nounroll
   for (int j = run.first; j < run.end; ++j) {
     __syncthreads();
-    if (j + 1 < run.end) load(j + 1);
+    if (j + 1 < run.end) {
+      load();
+      find_rows(j + 2);
+    }
     tile(tile_start(seen, j), buf);
-    if (j + 1 < run.end) stage(j + 1, buf ^ 1);
+    if (j + 1 < run.end) stage(tile_start(seen, j + 1), buf ^ 1);
     buf ^= 1;
   }
 
@@ -290,66 +345,71 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(4))) vo
     for (int j = run.first; j < run.end; ++j) {
       const int t0 = tile_start(seen, j);
       if (all_seen(wg_first, wg_last, t0, a.window, a.n_sink)) continue;
-      const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const SeenKeys sk = seen_keys(a, place[rb], seen.end, t0 + 8 * half);
 #pragma nounroll
-      for (int b = 0; b < 4; ++b) {
-        const int g = 2 * b + half;
-        const int row8 = t0 + 8 * g < seen.end ? group_row8(a.pages, table, kvh, t0 / 8 + g) : -1;
-        const uint32_t mask = row8 >= 0 ? seen_bits(sk, 16 * b) : 0u;
-        half8 ones;
+        for (int b = 0; b < 4; ++b) {
+          const int g = 2 * b + half;
+          const int row8 = t0 + 8 * g < seen.end ? group_row8(a.pages, table, kvh, t0 / 8 + g) : -1;
+          const uint32_t mask = row8 >= 0 ? seen_bits(sk, 16 * b) : 0u;
+          half8 ones;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ones[i] = (mask >> i) & 1 ? (_Float16)1.0f : (_Float16)0.0f;
+          for (int i = 0; i < 8; ++i) ones[i] = (mask >> i) & 1 ? (_Float16)1.0f : (_Float16)0.0f;
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 32 * nb + col), t0 + 8 * g, seen.end);
-          f32x16 n;
+          for (int nb = 0; nb < 2; ++nb) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 32 * nb + col), t0 + 8 * g, seen.end);
+            f32x16 n;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
-          n = __builtin_amdgcn_mfma_f32_32x32x16_f16(special_marks(v), ones, n, 0, 0, 0);
+            for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+            n = __builtin_amdgcn_mfma_f32_32x32x16_f16(special_marks(v), ones, n, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[nb][i] += special_sum(n[i]);
+            for (int i = 0; i < 16; ++i) acc[rb][nb][i] += special_sum(n[i]);
+          }
         }
       }
     }
   }
 
-  const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-  l = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
-  if (my_row >= rows) return;
-  if (S == 1) {
-    const int tok = my_row / a.G, head = a.q_head(kvh * a.G + (my_row - tok * a.G));
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int64_t base = ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * half;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[rb]), __float_as_uint(l[rb]), false, false);
+    l[rb] = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
+    const int row = wr0 + 32 * rb + col;
+    if (row >= rows) continue;
+    if (S == 1) {
+      const int tok = row / a.G, head = a.q_head(kvh * a.G + (row - tok * a.G));
+      const float inv = l[rb] == 0.0f ? 0.0f : 1.0f / l[rb];
+      const int64_t base = ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * half;
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          store_out4(a.out, base + 32 * nb + 8 * i, a.out_dtype, acc[rb][nb][4 * i] * inv,
+                     acc[rb][nb][4 * i + 1] * inv, acc[rb][nb][4 * i + 2] * inv, acc[rb][nb][4 * i + 3] * inv);
+      continue;
+    }
+    const float f = exact_reference(ref[rb], c[rb]);
+    float* part = a.many_part + ((((int64_t)index * Hkv + kvh) * S + split) * R + (row - r0)) * kPartial;
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        store_out4(a.out, base + 32 * nb + 8 * i, a.out_dtype, acc[nb][4 * i] * inv, acc[nb][4 * i + 1] * inv,
-                   acc[nb][4 * i + 2] * inv, acc[nb][4 * i + 3] * inv);
-    return;
+        *reinterpret_cast<f32x4*>(part + 32 * nb + 8 * i + 4 * half) =
+            f32x4{acc[rb][nb][4 * i] * f, acc[rb][nb][4 * i + 1] * f, acc[rb][nb][4 * i + 2] * f,
+                  acc[rb][nb][4 * i + 3] * f};
+    if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{ref[rb].m, l[rb] * f, c[rb], 0.0f};
   }
-  const float f = exact_reference(ref, c);
-  l *= f;
-  acc[0] *= f;
-  acc[1] *= f;
-  float* part = a.many_part + ((((int64_t)index * Hkv + kvh) * S + split) * R + (my_row - r0)) * kPartial;
-#pragma unroll
-  for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(part + 32 * nb + 8 * i + 4 * half) =
-          f32x4{acc[nb][4 * i], acc[nb][4 * i + 1], acc[nb][4 * i + 2], acc[nb][4 * i + 3]};
-  if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{ref.m, l, c, 0.0f};
 }
 
-template <int K, int VF, int NW>
+template <int K, int VF, int RB>
 hipError_t launch_many(const PagedAttendArgs& a, hipStream_t stream) {
   const dim3 grid((uint32_t)(a.plan.many_tiles * a.pages.Hkv * a.plan.many_splits));
   if (a.out_dtype == POT_FP32)
-    hipLaunchKernelGGL((paged_many_kernel<K, VF, NW, true>), grid, dim3(64 * NW), 0, stream, a);
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, RB, true>), grid, dim3(64 * kManyWaves), 0, stream, a);
   else
-    hipLaunchKernelGGL((paged_many_kernel<K, VF, NW, false>), grid, dim3(64 * NW), 0, stream, a);
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, RB, false>), grid, dim3(64 * kManyWaves), 0, stream, a);
   return hipGetLastError();
 }
 

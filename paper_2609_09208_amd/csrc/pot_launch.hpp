@@ -230,10 +230,10 @@ constexpr int kFewRows = 16;
 // many to a CU. uni: pages of whole tiles.
 constexpr int few_simd_waves(int mant_bits, bool uni) { return mant_bits == 0 && uni ? 4 : 3; }
 // How a call is split: the kernel of few rows in few_splits key ranges, the kernel of many in
-// tiles of 32 many_waves rows and many_splits ranges; splits of 0: not launched. Sequences of up
-// to few_limit rows go to the former.
+// tiles of many_rows (128 or 256) and many_splits ranges; splits of 0: not launched. Sequences of
+// up to few_limit rows go to the former.
 struct PagedPlan {
-  int32_t few_limit, few_splits, many_splits, many_waves;
+  int32_t few_limit, few_splits, many_splits, many_rows;
   int64_t many_tiles;  // an upper bound
 };
 // Floats of one row's partial: 64 sums, the reference, the weights' sum and the score factor.

@@ -138,7 +138,7 @@ def test_binding_refuses_host_tensors_and_other_shapes():
         with pytest.raises(pa.PotError):
             pa.make_pages(*bad)
     pages = _pages()
-    pages.tensors = (se, None, sc, v, table)
+    pages.calls = (3, -1, 0, 2)
     x = torch.zeros((3, 8, 64))
     with pytest.raises(pa.PotError):
         pa.pot_paged_attention(pa.make_format(), x, pages, table[:, 0], table[:, 0], HEADS[:8], 1, 16, x, None)
