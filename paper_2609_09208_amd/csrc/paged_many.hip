@@ -22,23 +22,23 @@ __global__ __launch_bounds__(256) void paged_many_merge_kernel(const PagedAttend
              g.o[2], g.o[3]);
 }
 
-template <int VF, int RB>
+template <int VF, int R>
 static hipError_t launch_k(const PagedAttendArgs& a, hipStream_t stream) {
   switch (a.mant_bits) {
-    case 0: return launch_many<0, VF, RB>(a, stream);
-    case 1: return launch_many<1, VF, RB>(a, stream);
-    case 2: return launch_many<2, VF, RB>(a, stream);
-    case 3: return launch_many<3, VF, RB>(a, stream);
-    default: return launch_many<4, VF, RB>(a, stream);
+    case 0: return launch_many<0, VF, R>(a, stream);
+    case 1: return launch_many<1, VF, R>(a, stream);
+    case 2: return launch_many<2, VF, R>(a, stream);
+    case 3: return launch_many<3, VF, R>(a, stream);
+    default: return launch_many<4, VF, R>(a, stream);
   }
 }
 
 hipError_t launch_paged_many(const PagedAttendArgs& a, hipStream_t stream) {
   const hipError_t e = a.plan.many_rows == 256
-                           ? (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 2>(a, stream)
-                                                                : launch_k<POT_VALUES_FP16, 2>(a, stream))
-                           : (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 1>(a, stream)
-                                                                : launch_k<POT_VALUES_FP16, 1>(a, stream));
+                           ? (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 256>(a, stream)
+                                                                : launch_k<POT_VALUES_FP16, 256>(a, stream))
+                           : (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 128>(a, stream)
+                                                                : launch_k<POT_VALUES_FP16, 128>(a, stream));
   if (e != hipSuccess || a.plan.many_splits == 1) return e;
   hipLaunchKernelGGL(paged_many_merge_kernel,
                      dim3((uint32_t)(a.plan.many_tiles * (a.plan.many_rows / 4)), (uint32_t)a.pages.Hkv),

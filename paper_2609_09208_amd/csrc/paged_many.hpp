@@ -70,21 +70,23 @@ struct ManyStage<POT_VALUES_INT4> {
   uint4 s, z;
 };
 
-constexpr int kManyWaves = 4;
+// Waves and row blocks a wave of the tiles of 128 and of 256 rows.
+constexpr int many_waves(int rows) { return rows == 256 ? 8 : 4; }
+constexpr int many_blocks(int rows) { return rows / 32 / many_waves(rows); }
 
-// RB: row blocks a wave. LOW: the weights' rounding goes into the products too (outputs of 32 bits).
-template <int K, int VF, int RB, bool LOW>
-__global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(RB == 2 ? 2 : 3)))
+// R: rows of a tile. LOW: the weights' rounding goes into the products too (outputs of 32 bits).
+template <int K, int VF, int R, bool LOW>
+__global__ __launch_bounds__(64 * many_waves(R)) __attribute__((amdgpu_waves_per_eu(many_waves(R) == 8 ? 4 : 3)))
 void paged_many_kernel(const PagedAttendArgs a) {
-  constexpr int NW = kManyWaves, R = 32 * RB * NW, kGroups = 8 / NW;  // groups a wave stages
+  constexpr int NW = many_waves(R), RB = many_blocks(R), kGroups = 8 / NW;  // groups a wave stages
   struct Tile {
-    uint4 k[8 * 64];  // chunk d (dimensions 8d ..+7) of key j at 64 d + (j ^ d)
+    uint4 k[8 * 65];  // chunk d (dimensions 8d ..+7) of key j at 65 d + j
     uint4 v[8 * 64];  // tokens 8g ..+7 of dimension d at 64 g + d
   };
   __shared__ Tile tiles[2];
   __shared__ __attribute__((aligned(16))) float scales[2][64];
   __shared__ __attribute__((aligned(16))) int flags[2][8];  // of a group: 1 not there, 2 holds special values
-  static_assert(sizeof(tiles) >= sizeof(uint4) * R * 8, "the queries pass through the tiles' place");
+  __shared__ uint4 queries[R * 9];  // chunk d of row r at 9 r + d; a wave's own rows
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int S = a.plan.many_splits, Hkv = a.pages.Hkv;
@@ -116,18 +118,20 @@ void paged_many_kernel(const PagedAttendArgs a) {
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
       st_row[i] = next_row[i];
-      const int64_t row8 = max(next_row[i], 0), row = row8 * 8 + (lane >> 3);
-      st[i].code = *reinterpret_cast<const uint32_t*>(a.pages.codes_se + row * 32 + 4 * (lane & 7));
+      // uniform, and said to be: addresses in scalar registers, a lane's offset once
+      const int64_t row8 = __builtin_amdgcn_readfirstlane(max(next_row[i], 0));
+      st[i].code = reinterpret_cast<const uint32_t*>(a.pages.codes_se + row8 * 256)[lane];
+      const uint8_t* planes = a.pages.codes_m + row8 * (64 * K);
 #pragma unroll
-      for (int p = 0; p < K; ++p) st[i].plane[p] = a.pages.codes_m[row * 8 * K + 8 * p + (lane & 7)];
-      st[i].scale = a.pages.key_scale[row8 * 8 + (lane & 7)];
+      for (int p = 0; p < K; ++p) st[i].plane[p] = planes[(uint32_t)((lane >> 3) * 8 * K + (lane & 7)) + 8 * p];
+      st[i].scale = (a.pages.key_scale + row8 * 8)[lane & 7];
       if constexpr (VF == POT_VALUES_INT4) {
         const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
-        st[i].n = *reinterpret_cast<const uint2*>(rec + 16 * (lane & 15) + 8 * (lane >> 5));
+        st[i].n = *reinterpret_cast<const uint2*>(rec + (uint32_t)(16 * (lane & 15) + 8 * (lane >> 5)));
         st[i].s = *reinterpret_cast<const uint4*>(rec + kI4Steps);
         st[i].z = *reinterpret_cast<const uint4*>(rec + kI4Minima);
       } else {
-        st[i].v = *reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim) + 16 * lane);
+        st[i].v = reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim))[lane];
       }
     }
   };
@@ -136,7 +140,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
       const int g = wave + NW * i, key = 8 * g + (lane >> 3), d = lane & 7;
-      tiles[buf].k[64 * d + (key ^ d)] = __builtin_bit_cast(uint4, paged_weights<K>(st[i].code, st[i].plane));
+      tiles[buf].k[65 * d + key] = __builtin_bit_cast(uint4, paged_weights<K>(st[i].code, st[i].plane));
       uint4 v;
       if constexpr (VF == POT_VALUES_INT4) {
         const int sh = (lane & 16) ? 4 : 0;
@@ -164,7 +168,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
   }
 
   // ---- queries: 8 rows of the wave at a time, 8 lanes each ---------------------------------
-  uint4* sq = reinterpret_cast<uint4*>(tiles) + wave * 32 * RB * 8;  // chunk d of row r at 8 r + (d ^ r % 8)
+  uint4* sq = queries + wave * 32 * RB * 9;
   float c[RB];
 #pragma unroll
   for (int i = 0; i < 4 * RB; ++i) {
@@ -175,20 +179,11 @@ void paged_many_kernel(const PagedAttendArgs a) {
       load8(a.q, (int64_t)(t.first + tok) * a.q_stride_t + head * a.q_stride_h, lane & 7, a.dtype, x);
     }
     float factor;
-    sq[rw * 8 + ((lane ^ rw) & 7)] = quantised_query(x, a.hadamard, lane, &factor);
+    sq[rw * 9 + (lane & 7)] = quantised_query(x, a.hadamard, lane, &factor);
     // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants that of rows col, 32 + col ..
     const float got = __shfl(factor, 8 * (col & 7), 64);
     if ((col >> 3) == (i & 3)) c[i >> 2] = got;
   }
-  __syncthreads();
-  half8 q[RB][4];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      q[rb][s] = __builtin_bit_cast(half8, sq[8 * (32 * rb + col) + ((2 * s + half) ^ (col & 7))]);
-  __syncthreads();
-
   const bool active = wr0 < rows;
   const int w_first = t.place + min(wr0, last) / a.G, w_last = t.place + min(wr0 + 32 * RB - 1, last) / a.G;
   int place[RB];
@@ -207,6 +202,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
   // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
   const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
 
+  const half2v kOnes = {(_Float16)1.0f, (_Float16)1.0f};
   auto compute = [&](bool part, int t0, int buf) {
     const Tile& T = tiles[buf];
     f32x16 s[RB][2];
@@ -219,10 +215,13 @@ void paged_many_kernel(const PagedAttendArgs a) {
 #pragma unroll
       for (int step = 0; step < 4; ++step) {
         const int d = 2 * step + half;
-        const half8 kv = __builtin_bit_cast(half8, T.k[64 * d + ((32 * kb + krow) ^ d)]);
+        const half8 kv = __builtin_bit_cast(half8, T.k[65 * d + 32 * kb + krow]);
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
-          s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q[rb][step], s[rb][kb], 0, 0, 0);
+        {
+          const half8 q = __builtin_bit_cast(half8, sq[9 * (32 * rb + col) + d]);
+          s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q, s[rb][kb], 0, 0, 0);
+        }
       }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -294,9 +293,13 @@ void paged_many_kernel(const PagedAttendArgs a) {
         for (int i = 0; i < 4; ++i) {
           const float p0 = weight_of(s[rb][kb][e0 + 2 * i], c[rb], shift[rb]);
           const float p1 = weight_of(s[rb][kb][e0 + 2 * i + 1], c[rb], shift[rb]);
-          l[rb] += p0;
-          l[rb] += p1;
           hi[rb][i] = pack_half(p0, p1);
+          if constexpr (LOW) {
+            l[rb] += p0;
+            l[rb] += p1;
+          } else {  // of the weights as they are multiplied
+            l[rb] = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[rb][i]), kOnes, l[rb], false);
+          }
           if constexpr (LOW) lo[rb][i] = low_part(p0, p1, hi[rb][i]);
         }
 #pragma unroll
@@ -403,13 +406,13 @@ void paged_many_kernel(const PagedAttendArgs a) {
   }
 }
 
-template <int K, int VF, int RB>
+template <int K, int VF, int R>
 hipError_t launch_many(const PagedAttendArgs& a, hipStream_t stream) {
   const dim3 grid((uint32_t)(a.plan.many_tiles * a.pages.Hkv * a.plan.many_splits));
   if (a.out_dtype == POT_FP32)
-    hipLaunchKernelGGL((paged_many_kernel<K, VF, RB, true>), grid, dim3(64 * kManyWaves), 0, stream, a);
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, R, true>), grid, dim3(64 * many_waves(R)), 0, stream, a);
   else
-    hipLaunchKernelGGL((paged_many_kernel<K, VF, RB, false>), grid, dim3(64 * kManyWaves), 0, stream, a);
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, R, false>), grid, dim3(64 * many_waves(R)), 0, stream, a);
   return hipGetLastError();
 }
 
