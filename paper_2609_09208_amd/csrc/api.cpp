@@ -638,22 +638,24 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
     p.many_rows = rows > 128 ? 256 : 128;
     const int64_t R = p.many_rows, full = ((int64_t)n * G + R - 1) / R;
     p.many_tiles = (int64_t)n * G / R + std::min(B, n);
-    const int64_t most = (tiles + 7) / 8;
-    p.many_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / (full * Hkv), most, 32}));
+    if (full * Hkv < kManyPieces && tiles > kManyRange) p.many_extra = (int32_t)(kManyPieces / Hkv);
   }
   return p;
 }
 
 struct PagedLayout {
-  size_t many, total;
+  size_t many, pieces, total;
 };
 PagedLayout paged_layout(const PagedPlan& p, int B, int Hkv) {
   PagedLayout w{};
   if (p.few_splits > 1)
     w.many = align_up((size_t)B * Hkv * p.few_splits * kFewRows * kPartial * 4, 256);
-  w.total = w.many;
-  if (p.many_splits > 1)
-    w.total += align_up((size_t)p.many_tiles * Hkv * p.many_splits * p.many_rows * kPartial * 4, 256);
+  w.pieces = w.total = w.many;
+  if (p.many_extra > 0) {
+    const size_t n = (size_t)(p.many_tiles + p.many_extra);
+    w.pieces += align_up(n * Hkv * p.many_rows * kPartial * 4, 256);
+    w.total = w.pieces + align_up(n * sizeof(int4), 256);
+  }
   return w;
 }
 
@@ -949,6 +951,7 @@ pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void*
   a.out = out;
   a.few_part = static_cast<float*>(workspace);
   a.many_part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.many);
+  a.many_pieces = reinterpret_cast<int4*>(static_cast<uint8_t*>(workspace) + w.pieces);
   a.Hq = Hq;
   a.G = Hq / pages->Hkv;
   a.max_new = max_new;
@@ -959,7 +962,7 @@ pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void*
   a.mant_bits = fmt->mant_bits;
   a.value_format = pages->value_format;
   hipError_t e = hipSuccess;
-  if (a.plan.many_splits > 0) e = launch_paged_many(a, static_cast<hipStream_t>(stream));
+  if (a.plan.many_tiles > 0) e = launch_paged_many(a, static_cast<hipStream_t>(stream));
   if (e == hipSuccess && a.plan.few_splits > 0) e = launch_paged_few(a, static_cast<hipStream_t>(stream));
   return hip_status(e, "paged attention launch");
 }

@@ -4,22 +4,27 @@
 
 namespace potattn {
 
-// The same merge for the rows of a row tile, a wave per row, four rows a workgroup.
+// The same merge for the rows of a row tile, a wave per row. A row tile's rows are shared out among its
+// pieces, kMergeParts workgroups for each.
+constexpr int kMergeParts = 4;
 __global__ __launch_bounds__(256) void paged_many_merge_kernel(const PagedAttendArgs a) {
-  const int R = a.plan.many_rows, S = a.plan.many_splits;
-  const int piece = blockIdx.x % (R / 4), kvh = blockIdx.y, index = blockIdx.x / (R / 4);
-  const RowTile at = find_tile(a, index, R);
-  if (at.b < 0) return;
-  const NewTokens t = sequence_tokens(a.packed, at.b, a.max_new, a.max_len);
-  const int lane = threadIdx.x & 63;
-  const int in = 4 * piece + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = at.tile * R + in;
-  if (r >= t.n * a.G) return;
-  const float* part = a.many_part + (((int64_t)index * a.pages.Hkv + kvh) * S * R + in) * kPartial;
-  const Merged g = merge_parts(part, R * kPartial, S, lane);
-  if (lane >= 16) return;
-  const int tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));
-  store_out4(a.out, ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * lane, a.out_dtype, g.o[0], g.o[1],
-             g.o[2], g.o[3]);
+  const int R = a.plan.many_rows, Hkv = a.pages.Hkv;
+  const int index = blockIdx.x / kMergeParts, kvh = blockIdx.y;
+  const int4 rec = a.many_pieces[index];
+  const int b = rec.x, tile = rec.y, S = rec.z, first = rec.w;
+  if (b < 0 || S <= 1) return;
+  const NewTokens t = sequence_tokens(a.packed, b, a.max_new, a.max_len);
+  const int lane = threadIdx.x & 63, rows = min(R, t.n * a.G - tile * R);
+  const int share = (index - first) * kMergeParts + blockIdx.x % kMergeParts, shares = S * kMergeParts;
+  const int end = min(rows, (share + 1) * R / shares);
+  const float* part = a.many_part + ((int64_t)first * Hkv + kvh) * R * kPartial;
+  for (int in = share * R / shares + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); in < end; in += 4) {
+    const Merged g = merge_parts(part + in * kPartial, Hkv * R * kPartial, S, lane);
+    if (lane >= 16) continue;
+    const int r = tile * R + in, tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));
+    store_out4(a.out, ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * lane, a.out_dtype, g.o[0], g.o[1],
+               g.o[2], g.o[3]);
+  }
 }
 
 template <int VF, int R>
@@ -39,9 +44,9 @@ hipError_t launch_paged_many(const PagedAttendArgs& a, hipStream_t stream) {
                                                                 : launch_k<POT_VALUES_FP16, 256>(a, stream))
                            : (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 128>(a, stream)
                                                                 : launch_k<POT_VALUES_FP16, 128>(a, stream));
-  if (e != hipSuccess || a.plan.many_splits == 1) return e;
+  if (e != hipSuccess || a.plan.many_extra == 0) return e;
   hipLaunchKernelGGL(paged_many_merge_kernel,
-                     dim3((uint32_t)(a.plan.many_tiles * (a.plan.many_rows / 4)), (uint32_t)a.pages.Hkv),
+                     dim3((uint32_t)((a.plan.many_tiles + a.plan.many_extra) * kMergeParts), (uint32_t)a.pages.Hkv),
                      dim3(256), 0, stream, a);
   return hipGetLastError();
 }

@@ -15,45 +15,86 @@
 
 namespace potattn {
 
-// Row tiles of a sequence.
-__device__ __forceinline__ int many_tiles_of(const PagedAttendArgs& a, int b, int R) {
-  if (b >= a.packed.B) return 0;
+// What a sequence asks for: its row tiles, and the 64-key tiles that the last of them sees.
+struct ManyShape {
+  int rows, keys;
+};
+__device__ __forceinline__ ManyShape many_shape(const PagedAttendArgs& a, int b, int R) {
+  if (b >= a.packed.B) return {0, 0};
   const NewTokens t = sequence_tokens(a.packed, b, a.max_new, a.max_len);
   const int rows = t.n * a.G;
-  return t.n <= a.plan.few_limit && rows <= a.plan.few_limit ? 0 : (rows + R - 1) / R;
+  if (t.n <= a.plan.few_limit && rows <= a.plan.few_limit) return {0, 0};
+  const int n = (rows + R - 1) / R;
+  return {n, max(1, seen_tiles(t.place + (n - 1) * R / a.G, t.place + t.n - 1, t.len, a.window, a.n_sink).tiles)};
 }
-// Tile i of all, counted from the last sequence's last: a prompt's late tiles, which see the
-// most keys, come first. b < 0: there is none. Every lane of the wave takes part.
-struct RowTile {
-  int b, tile;
+__device__ __forceinline__ int wave_scan(int v, int lane) {  // sums up to and with the lane's
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, 64);
+    v += lane >= o ? u : 0;
+  }
+  return v;
+}
+
+// A workgroup's piece: row tile `tile` of sequence b, key range `split` of `splits`. A row tile's
+// keys are split when the row tiles do not fill the chip (many_extra > 0): into ranges of equal
+// length for all sequences, the shortest (to the step) for which kManyPieces of them take the whole
+// work; a short sequence's rows stay whole. However the lengths fall, there are at most one piece a
+// row tile and many_extra more. Pieces count from the last sequence's last: a prompt's late tiles, which
+// see the most keys, come first. A row tile's pieces are first .. first + splits - 1. b < 0: there is
+// no piece i. Every lane of the wave takes part.
+struct RowPiece {
+  int b, tile, split, splits, first;
 };
-__device__ __forceinline__ RowTile find_tile(const PagedAttendArgs& a, int i, int R) {
+__device__ __forceinline__ RowPiece find_piece(const PagedAttendArgs& a, int i, int R) {
   const int lane = lane_id();
+  const ManyShape head = many_shape(a, lane, R);
+  auto shape = [&](int b0) { return b0 == 0 ? head : many_shape(a, b0 + lane, R); };
+  int range = 1 << 24;  // tiles
+  if (a.plan.many_extra > 0) {
+    int64_t work = 0;
+    for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
+      const ManyShape m = shape(b0);
+      work += (int64_t)m.rows * m.keys;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) work += __shfl_xor((long long)work, o, 64);
+    range = (int)min((int64_t)range, max((int64_t)kManyRange, (work + a.plan.many_extra - 1) / a.plan.many_extra));
+  }
   int total = 0;
-  for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
-    int n = many_tiles_of(a, b0 + lane, R);
+  auto ranges = [&](const ManyShape& m) { return (m.keys + range - 1) / range; };
+  for (int tries = 0;; ++tries) {
+    range = __builtin_amdgcn_readfirstlane(range);
+    int n = 0;
+    for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
+      const ManyShape m = shape(b0);
+      n += m.rows * ranges(m);
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
-    total += n;
+    total = __builtin_amdgcn_readfirstlane(n);
+    if (a.plan.many_extra == 0 || total <= a.plan.many_extra || tries == 5) break;
+    range += max(1, (int)((int64_t)range * (total - a.plan.many_extra) / a.plan.many_extra));
   }
-  i = __builtin_amdgcn_readfirstlane(total) - 1 - i;
-  if (i < 0) return {-1, 0};
+  i = total - 1 - i;
+  if (i < 0) return {-1, 0, 0, 0, 0};
+  int before = 0;  // pieces of the sequences before
   for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
-    const int n = many_tiles_of(a, b0 + lane, R);
-    int sum = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(sum, o, 64);
-      sum += lane >= o ? v : 0;
-    }
-    const uint64_t past = __ballot(sum > i);
+    const ManyShape m = shape(b0);
+    const int r = ranges(m), n = wave_scan(m.rows * r, lane);
+    const uint64_t past = __ballot(n > i);
     if (past != 0) {
       const int at = (int)__builtin_ctzll(past);
-      return {b0 + at, i - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(n, at))};
+      const int S = __builtin_amdgcn_readlane(r, at), tiles = __builtin_amdgcn_readlane(m.rows, at);
+      const int start = __builtin_amdgcn_readlane(n, at) - tiles * S;  // the sequence's first
+      const int tile = (i - start) / S;
+      return {b0 + at, tile, i - start - tile * S, S, total - (before + start + (tile + 1) * S)};
     }
-    i -= __builtin_amdgcn_readlane(sum, 63);
+    const int all = __builtin_amdgcn_readlane(n, 63);
+    i -= all;
+    before += all;
   }
-  return {-1, 0};
+  return {-1, 0, 0, 0, 0};
 }
 
 template <int VF>
@@ -89,16 +130,17 @@ void paged_many_kernel(const PagedAttendArgs a) {
   __shared__ uint4 queries[R * 9];  // chunk d of row r at 9 r + d; a wave's own rows
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int S = a.plan.many_splits, Hkv = a.pages.Hkv;
-  const int split = blockIdx.x % S, kvh = blockIdx.x / S % Hkv, index = blockIdx.x / S / Hkv;
-  const RowTile at = find_tile(a, index, R);
+  const int Hkv = a.pages.Hkv, kvh = blockIdx.x % Hkv, index = blockIdx.x / Hkv;
+  const RowPiece at = find_piece(a, index, R);
+  if (a.plan.many_extra > 0 && kvh == 0 && tid == 0)
+    a.many_pieces[index] = make_int4(at.b, at.tile, at.splits, at.first);
   if (at.b < 0) return;
   const NewTokens t = sequence_tokens(a.packed, at.b, a.max_new, a.max_len);
   const int rows = t.n * a.G, r0 = at.tile * R;
   const int last = min(r0 + R, rows) - 1;
   const int wg_first = t.place + r0 / a.G, wg_last = t.place + last / a.G;
   const SeenTiles seen = seen_tiles(wg_first, wg_last, t.len, a.window, a.n_sink);
-  const TileRun run = split_tiles(seen.tiles, split, S);
+  const TileRun run = split_tiles(seen.tiles, at.split, at.splits);
   const int32_t* table = a.pages.table + (int64_t)at.b * a.pages.table_len;
   const int col = lane & 31, half = lane >> 5;
   const int wr0 = r0 + 32 * RB * wave;  // the wave's first row
@@ -381,7 +423,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
     l[rb] = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
     const int row = wr0 + 32 * rb + col;
     if (row >= rows) continue;
-    if (S == 1) {
+    if (at.splits == 1) {
       const int tok = row / a.G, head = a.q_head(kvh * a.G + (row - tok * a.G));
       const float inv = l[rb] == 0.0f ? 0.0f : 1.0f / l[rb];
       const int64_t base = ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * half;
@@ -394,7 +436,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
       continue;
     }
     const float f = exact_reference(ref[rb], c[rb]);
-    float* part = a.many_part + ((((int64_t)index * Hkv + kvh) * S + split) * R + (row - r0)) * kPartial;
+    float* part = a.many_part + (((int64_t)index * Hkv + kvh) * R + (row - r0)) * kPartial;
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -408,7 +450,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
 
 template <int K, int VF, int R>
 hipError_t launch_many(const PagedAttendArgs& a, hipStream_t stream) {
-  const dim3 grid((uint32_t)(a.plan.many_tiles * a.pages.Hkv * a.plan.many_splits));
+  const dim3 grid((uint32_t)((a.plan.many_tiles + a.plan.many_extra) * a.pages.Hkv));
   if (a.out_dtype == POT_FP32)
     hipLaunchKernelGGL((paged_many_kernel<K, VF, R, true>), grid, dim3(64 * many_waves(R)), 0, stream, a);
   else

@@ -229,13 +229,15 @@ constexpr int kFewRows = 16;
 // Waves per SIMD that the kernel of few rows leaves registers for; its workgroups have four waves, so as
 // many to a CU. uni: pages of whole tiles.
 constexpr int few_simd_waves(int mant_bits, bool uni) { return mant_bits == 0 && uni ? 4 : 3; }
-// How a call is split: the kernel of few rows in few_splits key ranges, the kernel of many in
-// tiles of many_rows (128 or 256) and many_splits ranges; splits of 0: not launched. Sequences of
-// up to few_limit rows go to the former.
+// How a call is split: the kernel of few rows in few_splits key ranges (0: not launched), the kernel
+// of many in many_tiles tiles of many_rows (128 or 256; 0 tiles: not launched), which many_extra > 0
+// may split into that many pieces more a kv head. Sequences of up to few_limit rows go to the former.
 struct PagedPlan {
-  int32_t few_limit, few_splits, many_splits, many_rows;
+  int32_t few_limit, few_splits, many_rows, many_extra;
   int64_t many_tiles;  // an upper bound
 };
+// Key ranges of many rows: pieces that take the whole work together, and the shortest, in tiles.
+constexpr int kManyPieces = 512, kManyRange = 8;
 // Floats of one row's partial: 64 sums, the reference, the weights' sum and the score factor.
 constexpr int kPartial = 68;
 
@@ -244,7 +246,8 @@ struct PagedAttendArgs {
   int64_t q_stride_t, q_stride_h;  // elements
   void* out;
   float* few_part;   // [B][Hkv][few_splits][kFewRows][kPartial]
-  float* many_part;  // [tiles][Hkv][many_splits][rows of a tile][kPartial]
+  float* many_part;  // [pieces][Hkv][rows of a tile][kPartial]
+  int4* many_pieces;  // [pieces]: sequence, row tile, its pieces, the first of them
   PagesArg pages;
   PackedRows packed;
   PagedPlan plan;
