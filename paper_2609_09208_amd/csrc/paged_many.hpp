@@ -108,8 +108,13 @@ struct ManyStage<POT_VALUES_INT4> {
   uint32_t code, plane[4];
   float scale;
   uint2 n;
-  uint4 s, z;
+  uint32_t s, z;  // two of the 8 steps and minima, those of lane % 4
 };
+// The four lanes' dwords in each of them.
+__device__ __forceinline__ uint4 quad_dwords(uint32_t x) {
+  return make_uint4(__builtin_amdgcn_mov_dpp(x, 0x00, 0xF, 0xF, true), __builtin_amdgcn_mov_dpp(x, 0x55, 0xF, 0xF, true),
+                    __builtin_amdgcn_mov_dpp(x, 0xAA, 0xF, 0xF, true), __builtin_amdgcn_mov_dpp(x, 0xFF, 0xF, 0xF, true));
+}
 
 // Waves and row blocks a wave of the tiles of 128 and of 256 rows.
 constexpr int many_waves(int rows) { return rows == 256 ? 8 : 4; }
@@ -170,8 +175,8 @@ void paged_many_kernel(const PagedAttendArgs a) {
       if constexpr (VF == POT_VALUES_INT4) {
         const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
         st[i].n = *reinterpret_cast<const uint2*>(rec + (uint32_t)(16 * (lane & 15) + 8 * (lane >> 5)));
-        st[i].s = *reinterpret_cast<const uint4*>(rec + kI4Steps);
-        st[i].z = *reinterpret_cast<const uint4*>(rec + kI4Minima);
+        st[i].s = reinterpret_cast<const uint32_t*>(rec + kI4Steps)[lane & 3];
+        st[i].z = reinterpret_cast<const uint32_t*>(rec + kI4Minima)[lane & 3];
       } else {
         st[i].v = reinterpret_cast<const uint4*>(a.pages.values + row8 * (16 * kDim))[lane];
       }
@@ -186,7 +191,8 @@ void paged_many_kernel(const PagedAttendArgs a) {
       uint4 v;
       if constexpr (VF == POT_VALUES_INT4) {
         const int sh = (lane & 16) ? 4 : 0;
-        v = int4_values((st[i].n.x >> sh) & 0x0F0F0F0Fu, (st[i].n.y >> sh) & 0x0F0F0F0Fu, st[i].s, st[i].z);
+        v = int4_values((st[i].n.x >> sh) & 0x0F0F0F0Fu, (st[i].n.y >> sh) & 0x0F0F0F0Fu,
+                        quad_dwords(st[i].s), quad_dwords(st[i].z));
       } else {
         v = st[i].v;
       }
