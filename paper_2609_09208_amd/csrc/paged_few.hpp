@@ -34,10 +34,13 @@ __device__ __forceinline__ int lane_value(int v, int from) {
 }
 
 // UNI: a tile lies in one page (page sizes of whole tiles). LOW: the weights' rounding goes into
-// the products too (outputs of 32 bits).
-template <int K, int VF, bool UNI, bool LOW>
+// the products too (outputs of 32 bits). EIGHT: no sequence has more than 8 rows. The columns of the
+// products are 16 all the same, so columns 8 .. 15 take the same queries to a tile's other 32 keys:
+// scores K_0 [Q 0] + K_1 [0 Q], then half the scales, weights and references a lane; the weights meet
+// both halves' values, and of the two products a lane keeps its half's.
+template <int K, int VF, bool UNI, bool LOW, bool EIGHT>
 __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
-    few_simd_waves(K, UNI))))
+    few_simd_waves(K, UNI, EIGHT))))
 void paged_few_kernel(const PagedAttendArgs a) {
   constexpr int NW = kFewWaves, R = kFewRows;
   __shared__ uint4 sq[R][8];
@@ -53,6 +56,8 @@ void paged_few_kernel(const PagedAttendArgs a) {
   const TileRun run = split_tiles(seen.tiles, split, a.plan.few_splits);
   const int32_t* table = a.pages.table + (int64_t)b * a.pages.table_len;
   const int col = lane & 15, grp = lane >> 4;
+  constexpr int kHalves = EIGHT ? 1 : 2;  // half tiles that a lane has weights of
+  const int half = EIGHT ? col >> 3 : 0, query = EIGHT ? col & 7 : col;
 
   // The rows of a tile's groups: of the first one (UNI, uniform), or of group lane % 8 in each
   // lane; -1 where there is no page. Tiles past the run: the last one again.
@@ -69,7 +74,7 @@ void paged_few_kernel(const PagedAttendArgs a) {
   // 16 grp ..+15; scales and values of keys 32 kb + 8 grp ..+7
   uint2 kc[2][2];
   uint32_t kp[2][2][K > 0 ? K : 1];
-  float4 ks[2][2];
+  float4 ks[kHalves][2];
   FewValues<VF> vr;
   auto load_keys = [&](int rows8) {
 #pragma unroll
@@ -92,9 +97,12 @@ void paged_few_kernel(const PagedAttendArgs a) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const int64_t row8 = row_at(rows8, 4 * kb + grp);
-      const float4* sp = reinterpret_cast<const float4*>(a.pages.key_scale + row8 * 8);
-      ks[kb][0] = sp[0];
-      ks[kb][1] = sp[1];
+      if (kb < kHalves) {
+        const int64_t mine = EIGHT ? row_at(rows8, 4 * half + grp) : row8;
+        const float4* sp = reinterpret_cast<const float4*>(a.pages.key_scale + mine * 8);
+        ks[kb][0] = sp[0];
+        ks[kb][1] = sp[1];
+      }
       if constexpr (VF == POT_VALUES_INT4) {
         const uint8_t* rec = a.pages.values + row8 * kI4GroupBytes;
         vr.f[kb] = stream16(rec + 16 * col);
@@ -128,46 +136,55 @@ void paged_few_kernel(const PagedAttendArgs a) {
     if ((lane & 7) == 0) sc[r] = factor;
   }
   __syncthreads();
-  half8 q[2];
+  half8 q[3 - kHalves][2];  // of each half tile's keys
 #pragma unroll
-  for (int s = 0; s < 2; ++s) q[s] = __builtin_bit_cast(half8, sq[col][2 * grp + s]);
-  const float c = sc[col];
+  for (int s = 0; s < 2; ++s) {
+    const uint4 w = sq[query][2 * grp + s], none = make_uint4(0u, 0u, 0u, 0u);
+    q[0][s] = __builtin_bit_cast(half8, half == 0 ? w : none);
+    if constexpr (EIGHT) q[1][s] = __builtin_bit_cast(half8, half == 1 ? w : none);
+  }
+  const float c = sc[query];
 
-  f32x4 acc[4];
+  f32x4 acc[3 - kHalves][4];  // EIGHT: of either half tile's values
 #pragma unroll
-  for (int nb = 0; nb < 4; ++nb) acc[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int h = 0; h < 3 - kHalves; ++h)
+#pragma unroll
+    for (int nb = 0; nb < 4; ++nb) acc[h][nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   Reference ref;
   float l = 0.0f;
 
-  auto place_of_col = [&]() { return p_first + (col < rows ? col : 0) / a.G; };
+  auto place_of_col = [&]() { return p_first + (query < rows ? query : 0) / a.G; };
   bool special = false;  // a tile in part held special values (paged.hpp)
 
   auto tile = [&](auto part_tag, int t0) {
     constexpr bool PART = decltype(part_tag)::value;
-    float y[2][8];
+    float y[kHalves][8];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int s = 0; s < 2; ++s) {
+      f32x4 d[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t pl[K > 0 ? K : 1];
 #pragma unroll
           for (int p = 0; p < K; ++p) pl[p] = h ? kp[kb][s][p] >> 8 : kp[kb][s][p] & 0xFFu;
-          d = __builtin_amdgcn_mfma_f32_16x16x32_f16(paged_weights<K>(h ? kc[kb][s].y : kc[kb][s].x, pl),
-                                                     q[h], d, 0, 0, 0);
+          f32x4& at = d[EIGHT ? 0 : kb];
+          at = __builtin_amdgcn_mfma_f32_16x16x32_f16(paged_weights<K>(h ? kc[kb][s].y : kc[kb][s].x, pl),
+                                                      q[EIGHT ? kb : 0][h], at, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[kb][4 * s + i] = d[i];
-      }
+      for (int kb = 0; kb < kHalves; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[kb][4 * s + i] = d[kb][i];
+    }
     // the codes have become operands: the next tile's may come
     const int rows_tile = rows_now;
     load_keys(rows_next);
     rows_now = rows_next;
     rows_next = rows_of(j + 2 * NW);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < kHalves; ++kb)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const float4 sv = ks[kb][s];
@@ -182,15 +199,22 @@ void paged_few_kernel(const PagedAttendArgs a) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         const bool there = (UNI ? rows_tile : lane_value(rows_tile, 4 * kb + grp)) >= 0;
-        const uint32_t mask = there ? seen_bits(sk, 32 * kb) : 0u;
         end[kb] = there ? seen.end : 0;
+        if constexpr (!EIGHT) {
+          const uint32_t mask = there ? seen_bits(sk, 32 * kb) : 0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[kb][i] = if_seen(y[kb][i], mask, i);
+          for (int i = 0; i < 8; ++i) y[kb][i] = if_seen(y[kb][i], mask, i);
+        }
+      }
+      if constexpr (EIGHT) {
+        const uint32_t mask = end[half] > 0 ? seen_bits(sk, 32 * half) : 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[0][i] = if_seen(y[0][i], mask, i);
       }
     }
     float top = fmaxf(y[0][0], y[0][1]);
 #pragma unroll
-    for (int i = 2; i < 16; ++i) top = fmaxf(top, y[i >> 3][i & 7]);
+    for (int i = 2; i < 8 * kHalves; ++i) top = fmaxf(top, y[i >> 3][i & 7]);
     const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
@@ -198,30 +222,38 @@ void paged_few_kernel(const PagedAttendArgs a) {
     if (must_rise(ref, top, c)) {
       const float f = raise(ref, top, c);
 #pragma unroll
-      for (int nb = 0; nb < 4; ++nb) acc[nb] *= f;
+      for (int h = 0; h < 3 - kHalves; ++h)
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb) acc[h][nb] *= f;
       l *= f;
     }
     if (ref.far) {  // uniform
-      far_sums(ref, y[0]);
-      far_sums(ref, y[1]);
+#pragma unroll
+      for (int kb = 0; kb < kHalves; ++kb) far_sums(ref, y[kb]);
     }
     const float shift = weight_shift(ref);
-    uint32_t hi[2][4], lo[2][4];
+    uint32_t hi[kHalves][4], lo[kHalves][4];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < kHalves; ++kb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float p0 = weight_of(y[kb][2 * i], c, shift), p1 = weight_of(y[kb][2 * i + 1], c, shift);
-        l += p0;
-        l += p1;
         hi[kb][i] = pack_half(p0, p1);
+        if constexpr (LOW) {
+          l += p0;
+          l += p1;
+        } else {  // of the weights as they are multiplied
+          const half2v ones = {(_Float16)1.0f, (_Float16)1.0f};
+          l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[kb][i]), ones, l, false);
+        }
         if constexpr (LOW) lo[kb][i] = low_part(p0, p1, hi[kb][i]);
       }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[kb][0], hi[kb][1], hi[kb][2], hi[kb][3]));
+      const int at = EIGHT ? 0 : kb;  // of the weights
+      const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[at][0], hi[at][1], hi[at][2], hi[at][3]));
       half8 pl{};
-      if constexpr (LOW) pl = __builtin_bit_cast(half8, make_uint4(lo[kb][0], lo[kb][1], lo[kb][2], lo[kb][3]));
+      if constexpr (LOW) pl = __builtin_bit_cast(half8, make_uint4(lo[at][0], lo[at][1], lo[at][2], lo[at][3]));
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb) {
         uint4 u;
@@ -239,8 +271,9 @@ void paged_few_kernel(const PagedAttendArgs a) {
           u = without_special(u);
         }
         const half8 v = __builtin_bit_cast(half8, u);
-        acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph, acc[nb], 0, 0, 0);
-        if constexpr (LOW) acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, acc[nb], 0, 0, 0);
+        f32x4& sum = acc[EIGHT ? kb : 0][nb];
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph, sum, 0, 0, 0);
+        if constexpr (LOW) sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, sum, 0, 0, 0);
       }
     }
     load_values(rows_now);
@@ -279,7 +312,7 @@ void paged_few_kernel(const PagedAttendArgs a) {
           if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 16 * nb + col), t0 + 8 * g, seen.end);
           const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_f16(special_marks(v), ones, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[nb][i] += special_sum(n[i]);
+          for (int i = 0; i < 4; ++i) acc[0][nb][i] += special_sum(n[i]);  // EIGHT: those of half 0 count
         }
       }
     }
@@ -295,29 +328,36 @@ void paged_few_kernel(const PagedAttendArgs a) {
   const float f = exact_reference(ref, c);
   l *= f;
 #pragma unroll
-  for (int nb = 0; nb < 4; ++nb) acc[nb] *= f;
+  for (int nb = 0; nb < 4; ++nb) {
+    if constexpr (EIGHT) acc[0][nb] = half == 0 ? acc[0][nb] : acc[1][nb];
+    acc[0][nb] *= f;
+  }
   if (lane < R) {
     sm[wave][col] = ref.m;
     sl[wave][col] = l;
   }
 #pragma unroll
   for (int nb = 0; nb < 4; ++nb)
-    *reinterpret_cast<f32x4*>(&so[wave][col][16 * nb + 4 * grp]) = acc[nb];
+    *reinterpret_cast<f32x4*>(&so[wave][col][16 * nb + 4 * grp]) = acc[0][nb];
   __syncthreads();
   const int r = tid / 16, d = 4 * (tid & 15);
   if (r >= rows) return;
   const float cr = sc[r];
   float M = sm[0][r];
 #pragma unroll
-  for (int w = 1; w < NW; ++w) M = fmaxf(M, sm[w][r]);
+  for (int w = 0; w < NW; ++w)
+#pragma unroll
+    for (int h = 0; h < 3 - kHalves; ++h) M = fmaxf(M, sm[w][r + 8 * h]);
   float L = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    const float fw = between(sm[w][r], M, cr);
-    L += fw * sl[w][r];
-    o += fw * *reinterpret_cast<const f32x4*>(&so[w][r][d]);
-  }
+  for (int w = 0; w < NW; ++w)
+#pragma unroll
+    for (int h = 0; h < 3 - kHalves; ++h) {
+      const float fw = between(sm[w][r + 8 * h], M, cr);
+      L += fw * sl[w][r + 8 * h];
+      o += fw * *reinterpret_cast<const f32x4*>(&so[w][r + 8 * h][d]);
+    }
   if (a.plan.few_splits == 1) {
     const int tok = r / a.G, head = a.q_head(kvh * a.G + (r - tok * a.G));
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
@@ -330,16 +370,23 @@ void paged_few_kernel(const PagedAttendArgs a) {
   if (d == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{M, L, cr, 0.0f};
 }
 
+template <int K, int VF, bool UNI, bool LOW>
+void launch_few_rows(const PagedAttendArgs& a, dim3 grid, hipStream_t stream) {
+  if (a.plan.few_limit <= 8)
+    hipLaunchKernelGGL((paged_few_kernel<K, VF, UNI, LOW, true>), grid, dim3(64 * kFewWaves), 0, stream, a);
+  else
+    hipLaunchKernelGGL((paged_few_kernel<K, VF, UNI, LOW, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
+}
 template <int K, int VF>
 hipError_t launch_few(const PagedAttendArgs& a, hipStream_t stream) {
   const dim3 grid((uint32_t)a.plan.few_splits, (uint32_t)a.pages.Hkv, (uint32_t)a.packed.B);
   const bool uni = a.pages.page_groups % (kWTile / 8) == 0;
   if (a.out_dtype == POT_FP32) {
-    if (uni) hipLaunchKernelGGL((paged_few_kernel<K, VF, true, true>), grid, dim3(64 * kFewWaves), 0, stream, a);
-    else hipLaunchKernelGGL((paged_few_kernel<K, VF, false, true>), grid, dim3(64 * kFewWaves), 0, stream, a);
+    if (uni) launch_few_rows<K, VF, true, true>(a, grid, stream);
+    else launch_few_rows<K, VF, false, true>(a, grid, stream);
   } else {
-    if (uni) hipLaunchKernelGGL((paged_few_kernel<K, VF, true, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
-    else hipLaunchKernelGGL((paged_few_kernel<K, VF, false, false>), grid, dim3(64 * kFewWaves), 0, stream, a);
+    if (uni) launch_few_rows<K, VF, true, false>(a, grid, stream);
+    else launch_few_rows<K, VF, false, false>(a, grid, stream);
   }
   return hipGetLastError();
 }

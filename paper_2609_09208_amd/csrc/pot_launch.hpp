@@ -228,7 +228,7 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
 constexpr int kFewRows = 16;
 // Waves per SIMD that the kernel of few rows leaves registers for; its workgroups have four waves, so as
 // many to a CU. uni: pages of whole tiles.
-constexpr int few_simd_waves(int mant_bits, bool uni) { return mant_bits == 0 && uni ? 4 : 3; }
+constexpr int few_simd_waves(int mant_bits, bool uni, bool eight) { return mant_bits == 0 && uni && !eight ? 4 : 3; }
 // How a call is split: the kernel of few rows in few_splits key ranges (0: not launched), the kernel
 // of many in many_tiles tiles of many_rows (128 or 256; 0 tiles: not launched), which many_extra > 0
 // may split into that many pieces more a kv head. Sequences of up to few_limit rows go to the former.
