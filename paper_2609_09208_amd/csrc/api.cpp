@@ -620,7 +620,7 @@ pot_status check_head_groups(const int32_t* map, int Hq, int Hkv, uint32_t* q_of
 // How a paged attention call is split. A longer max_len never takes fewer splits than a shorter one or
 // a window, so that the workspace of the former serves the latter.
 PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, int window, int n_sink,
-                     int mant_bits, bool uni) {
+                     int mant_bits, bool uni, int value_format) {
   const int64_t G = Hq / Hkv, rows = std::min(max_new, n) * G;
   int64_t keys = max_len;  // that a row tile sees, at most
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + max_new + n_sink + 2 * kWTile);
@@ -630,8 +630,13 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
   // one sequence, or all of them as long as they may be: nothing is left for the kernel of few rows
   const bool both = many && G <= kFewRows && B > 1 && n < (int64_t)B * max_new;
   if (few || both) {
-    p.few_limit = (few ? rows : G) <= 8 ? 8 : kFewRows;
-    const int64_t units = (int64_t)B * Hkv, most = (tiles + 3) / 4;
+    p.few_limit = (few ? rows : G) <= 8 ? 8 : kFewRows;  // 8 rows have a form of their own
+    // Ranges of at least 4 tiles; where there is a workgroup for every CU without a split, of so many
+    // that the split repays its merge: 64 single tokens on 4096 keys of fp16 values 33 us in one range,
+    // 38 in two; of 1024 keys of 4-bit values 10.7 and 14.6, of 8192 42 and 40, and with lengths from
+    // 8192 down to 512 39 and 29.
+    const int64_t units = (int64_t)B * Hkv;
+    const int64_t most = units < 256 ? (tiles + 3) / 4 : tiles / (value_format == POT_VALUES_INT4 ? 32 : 64);
     const int per_cu = few_simd_waves(mant_bits, uni, p.few_limit == 8);
     p.few_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 * per_cu / units, most, 64}));
   }
@@ -905,7 +910,7 @@ size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, 
                                  int32_t max_len) {
   if (check_paged_sizes(B, n, Hq, Hkv, max_new, max_len) != POT_OK) return 0;
   if (B == 0 || n == 0) return 0;
-  return paged_layout(paged_plan(B, n, Hq, Hkv, max_new, max_len, 0, 0, 0, true), B, Hkv).total;
+  return paged_layout(paged_plan(B, n, Hq, Hkv, max_new, max_len, 0, 0, 0, true, POT_VALUES_INT4), B, Hkv).total;
 }
 
 pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void* q,
@@ -939,7 +944,7 @@ pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void*
   a.window = window >= (1 << 24) ? 0 : window;
   a.n_sink = std::min(n_sink, 1 << 24);
   a.plan = paged_plan(B, n, Hq, pages->Hkv, max_new, max_len, a.window, a.n_sink,
-                      fmt->mant_bits, pages->page_size % kWTile == 0);
+                      fmt->mant_bits, pages->page_size % kWTile == 0, pages->value_format);
   const PagedLayout w = paged_layout(a.plan, B, pages->Hkv);
   if (w.total > 0 && !workspace) return fail(POT_ERR_INVALID_ARG, "workspace is NULL");
   if (!aligned(workspace, 256))
