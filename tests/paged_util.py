@@ -116,10 +116,11 @@ def attend_bound(want, top, vmax, T, out):
     row scale's product, the difference from the reference, the last product and its sum): 6 2^-24 |x| in its exponent, ln 2 of
     that in a weight, twice (sums and denominator): under 2^-20 |x|. A weight's exp2 and its two fp16 parts: 2^-21 each, twice;
     fp32 sums of T terms in chains of at most T / 8 + 64: T 2^-27 + 2^-18. Outputs of 16 bits: the weights' one fp16 part, half a
-    step of fp16 (2^-11), and the output's own half step, of a number that may be that much larger."""
+    step of fp16 (d_i <= 2^-11 w_i) in both sums, so sum d_i (v_i - O) / sum w_i <= 2^-11 2 vmax; and the output's own half step,
+    of a number that may be that much larger."""
     e = vmax * (top * 2.0 ** -20 + 2.0 ** -19 + T * 2.0 ** -27 + 2.0 ** -18)
     if out != "fp32":
-        e = e + vmax * 2.0 ** -11
+        e = e + vmax * 2.0 ** -10
         e = e + (np.abs(want) + e) * HALF_STEP[out]
     return e
 
