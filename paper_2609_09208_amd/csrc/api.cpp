@@ -644,7 +644,7 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
     p.many_rows = rows > 128 ? 256 : 128;
     const int64_t R = p.many_rows, full = ((int64_t)n * G + R - 1) / R;
     p.many_tiles = (int64_t)n * G / R + std::min(B, n);
-    if (full * Hkv < kManyPieces && tiles > kManyRange) p.many_extra = (int32_t)(kManyPieces / Hkv);
+    if (full * Hkv < kManyPieces && tiles > kManyRange) p.many_extra = kManyPieces / Hkv;
   }
   return p;
 }

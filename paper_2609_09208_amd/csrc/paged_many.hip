@@ -38,12 +38,14 @@ static hipError_t launch_k(const PagedAttendArgs& a, hipStream_t stream) {
   }
 }
 
+template <int VF>
+static hipError_t launch_rows(const PagedAttendArgs& a, hipStream_t stream) {
+  return a.plan.many_rows == 256 ? launch_k<VF, 256>(a, stream) : launch_k<VF, 128>(a, stream);
+}
+
 hipError_t launch_paged_many(const PagedAttendArgs& a, hipStream_t stream) {
-  const hipError_t e = a.plan.many_rows == 256
-                           ? (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 256>(a, stream)
-                                                                : launch_k<POT_VALUES_FP16, 256>(a, stream))
-                           : (a.value_format == POT_VALUES_INT4 ? launch_k<POT_VALUES_INT4, 128>(a, stream)
-                                                                : launch_k<POT_VALUES_FP16, 128>(a, stream));
+  const hipError_t e = a.value_format == POT_VALUES_INT4 ? launch_rows<POT_VALUES_INT4>(a, stream)
+                                                         : launch_rows<POT_VALUES_FP16>(a, stream);
   if (e != hipSuccess || a.plan.many_extra == 0) return e;
   hipLaunchKernelGGL(paged_many_merge_kernel,
                      dim3((uint32_t)((a.plan.many_tiles + a.plan.many_extra) * kMergeParts), (uint32_t)a.pages.Hkv),

@@ -1,8 +1,7 @@
 // Attention over a paged cache for sequences with many rows (new tokens x query heads of a kv
-// head): chunks of prompts. A workgroup of four waves takes a tile of 128 RB rows of one sequence
-// and kv head, RB blocks of 32 rows a wave, and goes through the 64-key tiles that some of its rows
-// see; the keys' codes and the values become fp16 operands in LDS once for all its waves, the next
-// tile's loads under way meanwhile, and a wave reads them once for its RB blocks.
+// head): chunks of prompts. A workgroup takes a tile of R rows of one sequence and kv head, 32 a
+// wave, and goes through the 64-key tiles that some of its rows see; the keys' codes and the values
+// become fp16 operands in LDS once for all its waves, the next tile's loads under way meanwhile.
 //
 // Scores S^T = K Q^T by v_mfma_f32_32x32x16_f16 (codes as fp16 weights, the INT8 queries as fp16
 // integers: exact sums), the rows of K in such an order that a lane ends up with the scores of
@@ -116,15 +115,12 @@ __device__ __forceinline__ uint4 quad_dwords(uint32_t x) {
                     __builtin_amdgcn_mov_dpp(x, 0xAA, 0xF, 0xF, true), __builtin_amdgcn_mov_dpp(x, 0xFF, 0xF, 0xF, true));
 }
 
-// Waves and row blocks a wave of the tiles of 128 and of 256 rows.
-constexpr int many_waves(int rows) { return rows == 256 ? 8 : 4; }
-constexpr int many_blocks(int rows) { return rows / 32 / many_waves(rows); }
 
 // R: rows of a tile. LOW: the weights' rounding goes into the products too (outputs of 32 bits).
 template <int K, int VF, int R, bool LOW>
-__global__ __launch_bounds__(64 * many_waves(R)) __attribute__((amdgpu_waves_per_eu(many_waves(R) == 8 ? 4 : 3)))
+__global__ __launch_bounds__(2 * R) __attribute__((amdgpu_waves_per_eu(R == 128 ? 3 : 4)))
 void paged_many_kernel(const PagedAttendArgs a) {
-  constexpr int NW = many_waves(R), RB = many_blocks(R), kGroups = 8 / NW;  // groups a wave stages
+  constexpr int NW = R / 32, kGroups = 8 / NW;  // groups a wave stages
   struct Tile {
     uint4 k[8 * 65];  // chunk d (dimensions 8d ..+7) of key j at 65 d + j
     uint4 v[8 * 64];  // tokens 8g ..+7 of dimension d at 64 g + d
@@ -148,7 +144,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
   const TileRun run = split_tiles(seen.tiles, at.split, at.splits);
   const int32_t* table = a.pages.table + (int64_t)at.b * a.pages.table_len;
   const int col = lane & 31, half = lane >> 5;
-  const int wr0 = r0 + 32 * RB * wave;  // the wave's first row
+  const int wr0 = r0 + 32 * wave;  // the wave's first row
 
   // ---- staging: wave w has groups w, w + NW .. of the tile --------------------------------
   ManyStage<VF> st[kGroups];
@@ -188,6 +184,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
     for (int i = 0; i < kGroups; ++i) {
       const int g = wave + NW * i, key = 8 * g + (lane >> 3), d = lane & 7;
       tiles[buf].k[65 * d + key] = __builtin_bit_cast(uint4, paged_weights<K>(st[i].code, st[i].plane));
+      if (lane < 8) scales[buf][8 * g + lane] = st[i].scale;
       uint4 v;
       if constexpr (VF == POT_VALUES_INT4) {
         const int sh = (lane & 16) ? 4 : 0;
@@ -205,7 +202,6 @@ void paged_many_kernel(const PagedAttendArgs a) {
         }
       }
       tiles[buf].v[64 * g + lane] = v;
-      if (lane < 8) scales[buf][8 * g + lane] = st[i].scale;
       if (lane == 0) flags[buf][g] = flag;
     }
   };
@@ -216,10 +212,10 @@ void paged_many_kernel(const PagedAttendArgs a) {
   }
 
   // ---- queries: 8 rows of the wave at a time, 8 lanes each ---------------------------------
-  uint4* sq = queries + wave * 32 * RB * 9;
-  float c[RB];
+  uint4* sq = queries + wave * 32 * 9;
+  float c = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4 * RB; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const int rw = 8 * i + (lane >> 3), r = wr0 + rw;
     float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (r < rows) {
@@ -228,48 +224,36 @@ void paged_many_kernel(const PagedAttendArgs a) {
     }
     float factor;
     sq[rw * 9 + (lane & 7)] = quantised_query(x, a.hadamard, lane, &factor);
-    // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants that of rows col, 32 + col ..
+    // row 8 i + lane / 8 has its factor in 8 lanes; lane col wants that of row col
     const float got = __shfl(factor, 8 * (col & 7), 64);
-    if ((col >> 3) == (i & 3)) c[i >> 2] = got;
+    if ((col >> 3) == i) c = got;
   }
   const bool active = wr0 < rows;
-  const int w_first = t.place + min(wr0, last) / a.G, w_last = t.place + min(wr0 + 32 * RB - 1, last) / a.G;
-  int place[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) place[rb] = t.place + min(wr0 + 32 * rb + col, last) / a.G;
+  const int w_first = t.place + min(wr0, last) / a.G, w_last = t.place + min(wr0 + 31, last) / a.G;
+  const int place = t.place + min(wr0 + col, last) / a.G;
 
-  f32x16 acc[RB][2];
-  Reference ref[RB];
-  float l[RB];
+  f32x16 acc[2];
+  Reference ref;
+  float l = 0.0f;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[rb][0][i] = acc[rb][1][i] = 0.0f;
-    l[rb] = 0.0f;
-  }
+  for (int i = 0; i < 16; ++i) acc[0][i] = acc[1][i] = 0.0f;
   // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
   const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
 
   const half2v kOnes = {(_Float16)1.0f, (_Float16)1.0f};
   auto compute = [&](bool part, int t0, int buf) {
     const Tile& T = tiles[buf];
-    f32x16 s[RB][2];
+    f32x16 s[2];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[rb][0][i] = s[rb][1][i] = 0.0f;
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int step = 0; step < 4; ++step) {
         const int d = 2 * step + half;
         const half8 kv = __builtin_bit_cast(half8, T.k[65 * d + 32 * kb + krow]);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-        {
-          const half8 q = __builtin_bit_cast(half8, sq[9 * (32 * rb + col) + d]);
-          s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q, s[rb][kb], 0, 0, 0);
-        }
+        const half8 q = __builtin_bit_cast(half8, sq[9 * col + d]);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, q, s[kb], 0, 0, 0);
       }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -279,88 +263,59 @@ void paged_many_kernel(const PagedAttendArgs a) {
         const float4 a0 = sp[0], a1 = sp[1];
         const float sv[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[rb][kb][8 * u + i] *= sv[i];
+        for (int i = 0; i < 8; ++i) s[kb][8 * u + i] *= sv[i];
       }
     if (part) {  // uniform
+      const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const SeenKeys sk = seen_keys(a, place[rb], seen.end, t0 + 8 * half);
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t mask = flags[buf][4 * kb + 2 * u + half] & 1 ? 0u : seen_bits(sk, 32 * kb + 16 * u);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t mask = flags[buf][4 * kb + 2 * u + half] & 1 ? 0u : seen_bits(sk, 32 * kb + 16 * u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[rb][kb][8 * u + i] = if_seen(s[rb][kb][8 * u + i], mask, i);
-          }
-      }
+          for (int i = 0; i < 8; ++i) s[kb][8 * u + i] = if_seen(s[kb][8 * u + i], mask, i);
+        }
     }
-    float top[RB];
-    bool rises = false;
+    float top = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      top[rb] = fmaxf(s[rb][0][0], s[rb][0][1]);
-#pragma unroll
-      for (int i = 2; i < 32; ++i) top[rb] = fmaxf(top[rb], s[rb][i >> 4][i & 15]);
-      const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[rb]), __float_as_uint(top[rb]), false, false);
-      top[rb] = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
-      rises |= must_rise(ref[rb], top[rb], c[rb]);
+    for (int i = 2; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+    if (must_rise(ref, top, c)) {
+      const float f = raise(ref, top, c);
+      acc[0] *= f;
+      acc[1] *= f;
+      l *= f;
     }
-    bool far = false;
-    if (rises) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const float f = raise(ref[rb], top[rb], c[rb]);
-        acc[rb][0] *= f;
-        acc[rb][1] *= f;
-        l[rb] *= f;
-      }
+    if (ref.far) {  // uniform
+      s[0] -= ref.m;
+      s[1] -= ref.m;
     }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) far |= ref[rb].far;
-    if (far) {  // uniform
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const float off = ref[rb].far ? ref[rb].m : 0.0f;
-        s[rb][0] -= off;
-        s[rb][1] -= off;
-      }
-    }
-    float shift[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) shift[rb] = weight_shift(ref[rb]);
+    const float shift = weight_shift(ref);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {  // 16 keys at a time
       const int kb = b >> 1, e0 = 8 * (b & 1);
-      uint32_t hi[RB][4], lo[RB][4];
+      uint32_t hi[4], lo[4];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p0 = weight_of(s[rb][kb][e0 + 2 * i], c[rb], shift[rb]);
-          const float p1 = weight_of(s[rb][kb][e0 + 2 * i + 1], c[rb], shift[rb]);
-          hi[rb][i] = pack_half(p0, p1);
-          if constexpr (LOW) {
-            l[rb] += p0;
-            l[rb] += p1;
-          } else {  // of the weights as they are multiplied
-            l[rb] = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[rb][i]), kOnes, l[rb], false);
-          }
-          if constexpr (LOW) lo[rb][i] = low_part(p0, p1, hi[rb][i]);
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = weight_of(s[kb][e0 + 2 * i], c, shift), p1 = weight_of(s[kb][e0 + 2 * i + 1], c, shift);
+        hi[i] = pack_half(p0, p1);
+        if constexpr (LOW) {
+          l += p0;
+          l += p1;
+          lo[i] = low_part(p0, p1, hi[i]);
+        } else {  // of the weights as they are multiplied
+          l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[i]), kOnes, l, false);
         }
+      }
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb) {
         const half8 v = __builtin_bit_cast(half8, T.v[64 * (2 * b + half) + 32 * nb + col]);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[rb][0], hi[rb][1], hi[rb][2], hi[rb][3]));
-          acc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[rb][nb], 0, 0, 0);
-          if constexpr (LOW) {
-            const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[rb][0], lo[rb][1], lo[rb][2], lo[rb][3]));
-            acc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[rb][nb], 0, 0, 0);
-          }
+        const half8 ph = __builtin_bit_cast(half8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[nb], 0, 0, 0);
+        if constexpr (LOW) {
+          const half8 pl = __builtin_bit_cast(half8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+          acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[nb], 0, 0, 0);
         }
       }
     }
@@ -396,71 +351,64 @@ void paged_many_kernel(const PagedAttendArgs a) {
     for (int j = run.first; j < run.end; ++j) {
       const int t0 = tile_start(seen, j);
       if (all_seen(wg_first, wg_last, t0, a.window, a.n_sink)) continue;
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const SeenKeys sk = seen_keys(a, place[rb], seen.end, t0 + 8 * half);
+      const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
 #pragma nounroll
-        for (int b = 0; b < 4; ++b) {
-          const int g = 2 * b + half;
-          const int row8 = t0 + 8 * g < seen.end ? group_row8(a.pages, table, kvh, t0 / 8 + g) : -1;
-          const uint32_t mask = row8 >= 0 ? seen_bits(sk, 16 * b) : 0u;
-          half8 ones;
+      for (int b = 0; b < 4; ++b) {
+        const int g = 2 * b + half;
+        const int row8 = t0 + 8 * g < seen.end ? group_row8(a.pages, table, kvh, t0 / 8 + g) : -1;
+        const uint32_t mask = row8 >= 0 ? seen_bits(sk, 16 * b) : 0u;
+        half8 ones;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) ones[i] = (mask >> i) & 1 ? (_Float16)1.0f : (_Float16)0.0f;
+        for (int i = 0; i < 8; ++i) ones[i] = (mask >> i) & 1 ? (_Float16)1.0f : (_Float16)0.0f;
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 32 * nb + col), t0 + 8 * g, seen.end);
-            f32x16 n;
+        for (int nb = 0; nb < 2; ++nb) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row8 >= 0) v = mask_tokens(group_values<VF>(a.pages, row8, 32 * nb + col), t0 + 8 * g, seen.end);
+          f32x16 n;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) n[i] = 0.0f;
-            n = __builtin_amdgcn_mfma_f32_32x32x16_f16(special_marks(v), ones, n, 0, 0, 0);
+          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+          n = __builtin_amdgcn_mfma_f32_32x32x16_f16(special_marks(v), ones, n, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[rb][nb][i] += special_sum(n[i]);
-          }
+          for (int i = 0; i < 16; ++i) acc[nb][i] += special_sum(n[i]);
         }
       }
     }
   }
 
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[rb]), __float_as_uint(l[rb]), false, false);
-    l[rb] = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
-    const int row = wr0 + 32 * rb + col;
-    if (row >= rows) continue;
-    if (at.splits == 1) {
-      const int tok = row / a.G, head = a.q_head(kvh * a.G + (row - tok * a.G));
-      const float inv = l[rb] == 0.0f ? 0.0f : 1.0f / l[rb];
-      const int64_t base = ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * half;
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          store_out4(a.out, base + 32 * nb + 8 * i, a.out_dtype, acc[rb][nb][4 * i] * inv,
-                     acc[rb][nb][4 * i + 1] * inv, acc[rb][nb][4 * i + 2] * inv, acc[rb][nb][4 * i + 3] * inv);
-      continue;
-    }
-    const float f = exact_reference(ref[rb], c[rb]);
-    float* part = a.many_part + (((int64_t)index * Hkv + kvh) * R + (row - r0)) * kPartial;
+  const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
+  const int row = wr0 + col;
+  if (row >= rows) return;
+  if (at.splits == 1) {
+    const int tok = row / a.G, head = a.q_head(kvh * a.G + (row - tok * a.G));
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t base = ((int64_t)(t.first + tok) * a.Hq + head) * kDim + 4 * half;
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(part + 32 * nb + 8 * i + 4 * half) =
-            f32x4{acc[rb][nb][4 * i] * f, acc[rb][nb][4 * i + 1] * f, acc[rb][nb][4 * i + 2] * f,
-                  acc[rb][nb][4 * i + 3] * f};
-    if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{ref[rb].m, l[rb] * f, c[rb], 0.0f};
+        store_out4(a.out, base + 32 * nb + 8 * i, a.out_dtype, acc[nb][4 * i] * inv, acc[nb][4 * i + 1] * inv,
+                   acc[nb][4 * i + 2] * inv, acc[nb][4 * i + 3] * inv);
+    return;
   }
+  const float f = exact_reference(ref, c);
+  float* part = a.many_part + (((int64_t)index * Hkv + kvh) * R + (row - r0)) * kPartial;
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(part + 32 * nb + 8 * i + 4 * half) =
+          f32x4{acc[nb][4 * i] * f, acc[nb][4 * i + 1] * f, acc[nb][4 * i + 2] * f, acc[nb][4 * i + 3] * f};
+  if (half == 0) *reinterpret_cast<f32x4*>(part + kDim) = f32x4{ref.m, l * f, c, 0.0f};
 }
 
 template <int K, int VF, int R>
 hipError_t launch_many(const PagedAttendArgs& a, hipStream_t stream) {
   const dim3 grid((uint32_t)((a.plan.many_tiles + a.plan.many_extra) * a.pages.Hkv));
   if (a.out_dtype == POT_FP32)
-    hipLaunchKernelGGL((paged_many_kernel<K, VF, R, true>), grid, dim3(64 * many_waves(R)), 0, stream, a);
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, R, true>), grid, dim3(2 * R), 0, stream, a);
   else
-    hipLaunchKernelGGL((paged_many_kernel<K, VF, R, false>), grid, dim3(64 * many_waves(R)), 0, stream, a);
+    hipLaunchKernelGGL((paged_many_kernel<K, VF, R, false>), grid, dim3(2 * R), 0, stream, a);
   return hipGetLastError();
 }
 
