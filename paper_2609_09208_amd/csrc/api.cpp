@@ -630,7 +630,9 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
   // one sequence, or all of them as long as they may be: nothing is left for the kernel of few rows
   const bool both = many && G <= kFewRows && B > 1 && n < (int64_t)B * max_new;
   if (few || both) {
-    p.few_limit = (few ? rows : G) <= 8 ? 8 : kFewRows;  // 8 rows have a form of their own
+    // 8 rows have a form of their own (64 single tokens on 4096 keys 24.1 us, by the form of 16 rows
+    // 25.6); beside longer sequences those of 9 to 16 rows would go to the kernel of many for it
+    p.few_limit = few && rows <= 8 ? 8 : kFewRows;
     // Ranges of at least 4 tiles; where there is a workgroup for every CU without a split, of so many
     // that the split repays its merge: 64 single tokens on 4096 keys of fp16 values 33 us in one range,
     // 38 in two; of 1024 keys of 4-bit values 10.7 and 14.6, of 8192 42 and 40, and with lengths from
@@ -641,9 +643,10 @@ PagedPlan paged_plan(int B, int n, int Hq, int Hkv, int max_new, int max_len, in
     p.few_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 * per_cu / units, most, 64}));
   }
   if (many) {
-    p.many_rows = rows > 128 ? 256 : 128;
+    p.many_rows = rows > 128 ? 256 : 128;  // 64 sequences of 16 tokens, 8 heads each: 46 us by 128, 54 by 256
     const int64_t R = p.many_rows, full = ((int64_t)n * G + R - 1) / R;
     p.many_tiles = (int64_t)n * G / R + std::min(B, n);
+    // 512 rows of 8 heads on 8192 keys: 72 us with 512 pieces (two workgroups a CU), 92 with 256 or 1024
     if (full * Hkv < kManyPieces && tiles > kManyRange) p.many_extra = kManyPieces / Hkv;
   }
   return p;

@@ -4,7 +4,10 @@
 // the same 8 lanes in all three steps).
 //
 // Bound: the stream of many tokens (rows in, queries out: 9/10 of the bytes at 32 + 4 + 4 heads);
-// of few a chain of round trips: the sequence's bounds, its length and page, the row.
+// of few a chain of round trips: the sequence's bounds, its length and page, the row. Measured (32 + 4 + 4
+// heads): 1 token 5 us, 64 sequences of one 6, 8192 tokens bf16 to k = 4 and fp16 values 19.5 (97 MB with what
+// reads them back: 4 TB/s); 2300 tokens of fp32 with rotated keys, k = 2, 16 + 8 + 8 heads, 15.5 (VALU: the
+// encoder's divisions and both rotations).
 #include "encode_rows.hpp"
 #include "head_rows.hpp"
 #include "paged.hpp"
@@ -299,8 +302,10 @@ __global__ __launch_bounds__(64) void paged_append_heads_kernel(const PagedAppen
     store_value(a, halves, row8, t.place & 7, lane, there && kind == 2 && first >= 0, false);
 }
 
-// Which kernel: as for norm and rotation alone.
-constexpr int kManyTokens = 1024;
+// Which kernel (32 + 4 + 4 heads, 4-bit values): 512 tokens 9.6 us by tokens and 9.8 by heads, 1000 10.7 and
+// 11.5, 4000 17.7 and 24.4. Waves of the former: 8192 tokens, k = 4, with fp16 values, read back, 25.0 us with
+// 4096, 27.1 with 2048, 28.7 with 8192.
+constexpr int kManyTokens = 512;
 constexpr int kTargetWaves = 4096;
 
 template <int K, int MODE>
