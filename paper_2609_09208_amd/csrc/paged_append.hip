@@ -22,17 +22,26 @@ struct Token {
 };
 // Row t0 + `in` of a wave's rows t0 .. t0 + N - 1 (`in` differs by lane, 0 .. N - 1). Every lane
 // takes part: a lane reads one sequence's end, and a row's sequence is the number of ends at or
-// before it.
+// before it. Of more than 64 sequences, 64 ends find the part that row t0's is in, and so on.
 template <int N>
 __device__ __forceinline__ Token find_token(const PackedRows& r, int t0, int in, int lane) {
-  int before = 0;
-  for (int b0 = 0; b0 < r.B; b0 += 64) {
+  int first = 0;  // sequences that end at or before row t0, at least
+  for (int span = r.B; span > 64;) {
+    const int step = (span + 63) / 64, e = min(first + (lane + 1) * step, r.B);  // ascending
+    const int n = (int)__builtin_popcountll(__ballot(r.cu_new[e] <= t0));
+    first = min(first + n * step, r.B);
+    span = min(step, r.B - first);
+  }
+  int before = first;
+  for (int b0 = first; b0 < r.B; b0 += 64) {
     const int b = b0 + lane, end = b < r.B ? r.cu_new[b + 1] : INT32_MAX;
+    uint64_t past = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int n = (int)__builtin_popcountll(__ballot(b < r.B && end <= t0 + i));
-      before += in == i ? n : 0;
+      past = __ballot(b < r.B && end <= t0 + i);
+      before += in == i ? (int)__builtin_popcountll(past) : 0;
     }
+    if (past != ~0ull) break;
   }
   const int tok = t0 + in;
   if (tok >= r.n || before >= r.B || tok < r.cu_new[before]) return {-1, -1};

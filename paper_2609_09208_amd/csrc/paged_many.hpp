@@ -48,59 +48,77 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {  // sums up to and w
 // work; a short sequence's rows stay whole. However the lengths fall, there are at most one piece a
 // row tile and many_extra more. Pieces count from the last sequence's last: a prompt's late tiles, which
 // see the most keys, come first. A row tile's pieces are first .. first + splits - 1. b < 0: there is
-// no piece i. Every lane of the wave takes part.
+// no piece i. Every thread of the workgroup takes part, a sequence a thread.
 struct RowPiece {
   int b, tile, split, splits, first;
 };
-__device__ __forceinline__ RowPiece find_piece(const PagedAttendArgs& a, int i, int R) {
-  const int lane = lane_id();
-  const ManyShape head = many_shape(a, lane, R);
-  auto shape = [&](int b0) { return b0 == 0 ? head : many_shape(a, b0 + lane, R); };
+template <int NW>
+struct FindScratch {
+  int64_t sums[NW];
+  RowPiece found;
+};
+template <int NW>
+__device__ __forceinline__ RowPiece find_piece(const PagedAttendArgs& a, int i, int R, FindScratch<NW>& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const ManyShape mine = many_shape(a, tid, R);
+  auto shape = [&](int b0) { return b0 == 0 ? mine : many_shape(a, b0 + tid, R); };
+  auto over_group = [&](int64_t v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor((long long)v, o, 64);
+    if (lane == 0) sh.sums[wave] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += sh.sums[w];
+    __syncthreads();
+    return v;
+  };
+  const int extra = a.plan.many_extra;
   int range = 1 << 24;  // tiles
-  if (a.plan.many_extra > 0) {
+  if (extra > 0) {
     int64_t work = 0;
-    for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
+    for (int b0 = 0; b0 < a.packed.B; b0 += 64 * NW) {
       const ManyShape m = shape(b0);
       work += (int64_t)m.rows * m.keys;
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) work += __shfl_xor((long long)work, o, 64);
-    range = (int)min((int64_t)range, max((int64_t)kManyRange, (work + a.plan.many_extra - 1) / a.plan.many_extra));
+    // half a piece a row tile is lost by rounding up, of as many as the call's rows make
+    const int64_t most = extra - min((int64_t)extra, (int64_t)a.packed.n * a.G / R) / 2;
+    range = (int)min((int64_t)range, max((int64_t)kManyRange, (over_group(work) + most - 1) / most));
   }
-  int total = 0;
-  auto ranges = [&](const ManyShape& m) { return (m.keys + range - 1) / range; };
+  auto pieces = [&](const ManyShape& m) { return m.rows * ((m.keys + range - 1) / range); };
+  int64_t total = 0;
   for (int tries = 0;; ++tries) {
-    range = __builtin_amdgcn_readfirstlane(range);
-    int n = 0;
-    for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
-      const ManyShape m = shape(b0);
-      n += m.rows * ranges(m);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
-    total = __builtin_amdgcn_readfirstlane(n);
-    if (a.plan.many_extra == 0 || total <= a.plan.many_extra || tries == 5) break;
-    range += max(1, (int)((int64_t)range * (total - a.plan.many_extra) / a.plan.many_extra));
+    int64_t n = 0;
+    for (int b0 = 0; b0 < a.packed.B; b0 += 64 * NW) n += pieces(shape(b0));
+    total = over_group(n);
+    if (extra == 0 || total <= extra || tries == 5) break;
+    range += max(1, (int)(range * (total - extra) / extra));
   }
-  i = total - 1 - i;
-  if (i < 0) return {-1, 0, 0, 0, 0};
-  int before = 0;  // pieces of the sequences before
-  for (int b0 = 0; b0 < a.packed.B; b0 += 64) {
+  if (tid == 0) sh.found.b = -1;
+  const int64_t at = total - 1 - i;
+  int64_t before = 0;  // pieces of the sequences before
+  for (int b0 = 0; b0 < a.packed.B && at >= before; b0 += 64 * NW) {  // uniform
     const ManyShape m = shape(b0);
-    const int r = ranges(m), n = wave_scan(m.rows * r, lane);
-    const uint64_t past = __ballot(n > i);
-    if (past != 0) {
-      const int at = (int)__builtin_ctzll(past);
-      const int S = __builtin_amdgcn_readlane(r, at), tiles = __builtin_amdgcn_readlane(m.rows, at);
-      const int start = __builtin_amdgcn_readlane(n, at) - tiles * S;  // the sequence's first
-      const int tile = (i - start) / S;
-      return {b0 + at, tile, i - start - tile * S, S, total - (before + start + (tile + 1) * S)};
+    const int n = pieces(m), sum = wave_scan(n, lane);
+    if (lane == 63) sh.sums[wave] = sum;
+    __syncthreads();
+    int64_t start = before + sum - n;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      start += w < wave ? sh.sums[w] : 0;
+      before += sh.sums[w];
     }
-    const int all = __builtin_amdgcn_readlane(n, 63);
-    i -= all;
-    before += all;
+    if (at >= start && at < start + n) {
+      const int S = n / m.rows, j = (int)(at - start), tile = j / S;
+      sh.found = {b0 + tid, tile, j - tile * S, S, (int)(total - (start + (int64_t)(tile + 1) * S))};
+    }
+    __syncthreads();
   }
-  return {-1, 0, 0, 0, 0};
+  __syncthreads();
+  const RowPiece p = sh.found;
+  return {__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.tile),
+          __builtin_amdgcn_readfirstlane(p.split), __builtin_amdgcn_readfirstlane(p.splits),
+          __builtin_amdgcn_readfirstlane(p.first)};
 }
 
 template <int VF>
@@ -139,7 +157,8 @@ void paged_many_kernel(const PagedAttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int Hkv = a.pages.Hkv, kvh = blockIdx.x % Hkv, index = blockIdx.x / Hkv;
-  const RowPiece at = find_piece(a, index, R);
+  __shared__ FindScratch<NW> scratch;
+  const RowPiece at = find_piece(a, index, R, scratch);
   if (a.plan.many_extra > 0 && kvh == 0 && tid == 0)
     a.many_pieces[index] = make_int4(at.b, at.tile, at.splits, at.first);
   if (at.b < 0) return;
@@ -244,11 +263,17 @@ void paged_many_kernel(const PagedAttendArgs a) {
   float l = 0.0f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[0][i] = acc[1][i] = 0.0f;
-  // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
-  const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
 
   const half2v kOnes = {(_Float16)1.0f, (_Float16)1.0f};
   auto compute = [&](bool part, int t0, int buf) {
+    // Places in LDS. Where a tile's loads take the most registers they are made anew for each tile: kept
+    // through the loop, they leave reloads from memory behind the loads under way (2048 tokens with a window of
+    // 1000, k = 4, 4 bits: 81 us against 84; at k = 1 and fp16 values 432 against 426).
+    int ln = lane;
+    if constexpr (K > 0 && VF == POT_VALUES_INT4) asm volatile("" : "+v"(ln));
+    const int col = ln & 31, half = ln >> 5;
+    // row of K for the lane: key 16 (col / 16) + 8 (col / 4 % 2) + 4 (col / 8 % 2) + col % 4
+    const int krow = (col & 16) | ((col & 4) << 1) | ((col & 8) >> 1) | (col & 3);
     const Tile& T = tiles[buf];
     f32x16 s[2];
 #pragma unroll

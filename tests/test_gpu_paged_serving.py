@@ -212,3 +212,40 @@ def test_pages_past_32_bits(int4):
     assert torch.equal(*got) and bool(torch.isfinite(got[0]).all())
     for big, t in ((se, small.se), (sc, small.sc), (v, small.vals)):
         assert torch.equal(big[n_big - n_pages:].view(torch.uint8), t.view(torch.uint8))
+
+
+@pytest.mark.parametrize("B", [65, 1000, 5000])
+def test_many_sequences(B):
+    """Chunks and tokens among thousands of sequences, some without new tokens: rows find their sequences."""
+    rng = np.random.default_rng(11)
+    news = rng.choice([0, 1, 1, 1, 2], B)
+    news[rng.integers(0, B, 3)] = [40, 17, 33]
+    news[-1] = 0
+    lens = [int(n) + int(x) for n, x in zip(news, rng.integers(0, 30, B))]
+    lens[int(np.argmax(news))] += 2000
+    Hq, Hkv, page = 4, 1, 8
+    table, n_pages = make_table(rng, lens, page)
+    pool = Pool(rng, n_pages, Hkv, page, 0, True, False, table)
+    n = int(news.sum())
+    x = torch.from_numpy(rng.standard_normal((n, Hq + 2 * Hkv, 64)).astype(np.float32)).to(DEV)
+    cu, ls = _dev(bounds_of(news)), _dev(lens)
+    q = torch.empty((n, Hq, 64), device=DEV)
+    for t in (pool.sc, pool.vals, pool.se):
+        t.zero_()
+    pa.pot_paged_append(pool.fmt, pa.make_rope(0), x[:, :Hq], x[:, Hq:Hq + 1], x[:, Hq + 1:], None, None, 1e-6, None, None,
+                        pool.pages, cu, ls, q)
+    assert torch.equal(q, x[:, :Hq])
+    # the rows' places in the pool, from the definition
+    row = []
+    for b, (m, L) in enumerate(zip(news, lens)):
+        t = np.arange(L - m, L)
+        row.append(table[b, t // page] * page + t % page)
+    row = np.concatenate(row).astype(np.int64)
+    want = torch.zeros(n_pages * page, 64, dtype=torch.float16, device=DEV)
+    want[torch.from_numpy(row).to(DEV)] = x[:, Hq].half()
+    scales = pool.sc.reshape(-1).clone()
+    pa.pot_encode_keys(pool.fmt, want, n_pages * page, 1, 0, pool.sc, pool.se, None)
+    mine = torch.zeros_like(scales, dtype=torch.bool)
+    mine[torch.from_numpy(row).to(DEV)] = True
+    assert torch.equal(scales[mine], pool.sc.reshape(-1)[mine]) and (scales[~mine] == 0).all()
+    check_attend(pool, q, [int(m) for m in news], lens, _heads(Hq, Hkv))
