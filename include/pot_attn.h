@@ -380,7 +380,8 @@ size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, 
  * sums, here by codes decoded to fp16 weights on the matrix cores) and v_j the fp16 numbers that
  * the cache stands for: as stored, or z + s n rounded once to fp16. Sums are fp32; weights enter
  * the value products as fp16 numbers rounded to nearest, for outputs of 32 bits with what the
- * rounding left added. A query that sees no key gets O = 0. What is not seen (later tokens, tokens
+ * rounding left added, and for outputs of 16 bits the denominator is their sum as they are. A query
+ * that sees no key gets O = 0. What is not seen (later tokens, tokens
  * outside the window, rows past a sequence's end, infinities and NaN there) never reaches O; an
  * infinite or NaN value that is seen makes its element of O infinite or NaN (which is not defined).
  * Scores, in the log2 domain, may lie anywhere in fp32's range.
