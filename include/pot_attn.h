@@ -399,7 +399,8 @@ size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, 
  *  out          dense [n][Hq][64], device, 16-byte aligned; may not alias q or the cache.
  *  workspace    >= pot_paged_workspace_bytes(...) bytes, 256-byte aligned; any contents. Calls that
  *               share one must not overlap in time.
- * Results do not differ from call to call. B or n of 0 is a no-op. n up to 2^23, B up to 65535. */
+ * Results do not differ from call to call. B or n of 0 is a no-op. n up to 2^23, B up to 65535, and
+ * n * Hq / 256 + B * Hkv below 2^23 - 512. */
 pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void* q,
                                int64_t stride_t, int64_t stride_h, const pot_pages* pages,
                                const int32_t* cu_new, const int32_t* seq_lens,

@@ -597,6 +597,10 @@ pot_status check_paged_sizes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, int3
   if (Hq > kMaxHqArg) return fail(POT_ERR_UNSUPPORTED, "Hq %d > %d", Hq, kMaxHqArg);
   if (Hq % Hkv) return fail(POT_ERR_UNSUPPORTED, "Hq %d not a multiple of Hkv %d", Hq, Hkv);
   if (max_len > kMaxKeys) return fail(POT_ERR_UNSUPPORTED, "max_len %d > %d", max_len, kMaxKeys);
+  // a launch has fewer than 2^32 threads: 512 for 256 rows of a kv head, and for each sequence's last ones
+  if ((int64_t)n * Hq / 256 + (int64_t)std::min(B, n) * Hkv >= (1 << 23) - kManyPieces)
+    return fail(POT_ERR_UNSUPPORTED, "%d rows of %d heads in %d sequences of %d kv heads: too many for a launch", n, Hq, B,
+                Hkv);
   return POT_OK;
 }
 

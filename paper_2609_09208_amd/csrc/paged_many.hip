@@ -12,7 +12,10 @@ __global__ __launch_bounds__(256) void paged_many_merge_kernel(const PagedAttend
   const int index = blockIdx.x / kMergeParts, kvh = blockIdx.y;
   const int4 rec = a.many_pieces[index];
   const int b = rec.x, tile = rec.y, S = rec.z, first = rec.w;
-  if (b < 0 || S <= 1) return;
+  // bounds that do not ascend can ask for more pieces than there is room for
+  if (b < 0 || S <= 1 || first < 0 || index < first || index >= first + S ||
+      first + S > a.plan.many_tiles + a.plan.many_extra)
+    return;
   const NewTokens t = sequence_tokens(a.packed, b, a.max_new, a.max_len);
   const int lane = threadIdx.x & 63, rows = min(R, t.n * a.G - tile * R);
   const int share = (index - first) * kMergeParts + blockIdx.x % kMergeParts, shares = S * kMergeParts;

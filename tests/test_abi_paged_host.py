@@ -144,3 +144,13 @@ def test_binding_refuses_host_tensors_and_other_shapes():
         pa.pot_paged_attention(pa.make_format(), x, pages, table[:, 0], table[:, 0], HEADS[:8], 1, 16, x, None)
     with pytest.raises(pa.PotError):
         pa.pot_paged_append(pa.make_format(), pa.make_rope(), x, x, x, None, None, 0.0, None, None, pages, table, table, x)
+
+
+def test_calls_too_large_for_a_launch():
+    w = pa.pot_paged_workspace_bytes
+    for B, n, Hq, Hkv in [(65535, 1 << 23, 128, 128), (65535, 65535 * 2, 128, 128), (65535, 1 << 23, 128, 64)]:
+        assert w(B, n, Hq, Hkv, 300, 5000) == 0
+        assert _attend(B=B, n=n, Hq=Hq, max_new=300, pages=_pages(Hkv=Hkv)) == UNSUPPORTED
+    for B, n, Hkv in [(65535, 65535 * 2, 8), (1, 1 << 23, 8), (65535, 1 << 23, 16)]:  # refused for q, not for the sizes
+        assert _attend(B=B, n=n, Hq=128, max_new=300, heads=(np.arange(128) // (128 // Hkv)).astype(np.int32),
+                       pages=_pages(Hkv=Hkv), q=None) == INVALID

@@ -214,6 +214,23 @@ def test_pages_past_32_bits(int4):
         assert torch.equal(big[n_big - n_pages:].view(torch.uint8), t.view(torch.uint8))
 
 
+@pytest.mark.parametrize("B,n,cu", [(41, 300, [0, 300] * 21), (4, 300, [0, 300, -7, 10 ** 9, 3]), (3, 40, [50, 20, 40, 10])])
+def test_bounds_that_do_not_ascend(B, n, cu):
+    """Nonsense in the bounds: nothing outside out and the workspace changes, and other calls go on."""
+    rng = np.random.default_rng(12)
+    lens = [4000] * B
+    table, n_pages = make_table(rng, [4000], 64)
+    pool = Pool(rng, n_pages, 1, 64, 0, True, False, np.repeat(table, B, 0))
+    q = torch.from_numpy(rng.standard_normal((n, 8, 64)).astype(np.float32)).to(DEV)
+    size = pa.pot_paged_workspace_bytes(B, n, 8, 1, 300, 4000)
+    ws = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    wide = torch.full((n + 64, 8, 64), 7.5, device=DEV)
+    pa.pot_paged_attention(pool.fmt, q, pool.pages, _dev(cu), _dev(lens), _heads(8, 1), 300, 4000, wide[32:32 + n], ws[:size])
+    torch.cuda.synchronize()
+    assert (ws[size:] == 0x5A).all() and (wide[:32] == 7.5).all() and (wide[32 + n:] == 7.5).all()
+    check_attend(pool, q[:40].contiguous(), [40] + [0] * (B - 1), lens, _heads(8, 1))
+
+
 @pytest.mark.parametrize("B", [65, 1000, 5000])
 def test_many_sequences(B):
     """Chunks and tokens among thousands of sequences, some without new tokens: rows find their sequences."""
