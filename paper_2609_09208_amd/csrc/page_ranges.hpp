@@ -90,4 +90,42 @@ POT_BOTH constexpr TileRun split_tiles(int tiles, int split, int n_splits) {
   return {first, first + per < tiles ? first + per : tiles};
 }
 
+// Key ranges of row tiles with many rows. A sequence of `rows` row tiles that see up to `keys` key tiles
+// makes a piece for each row tile and range of `range` key tiles; the shortest range and the longest
+// (of no split), in tiles.
+constexpr int kManyRange = 8, kNoSplit = 1 << 24;
+POT_BOTH constexpr int pieces_of(int rows, int keys, int range) {
+  return rows * ((keys + range - 1) / range);
+}
+// The range for a call that may split its row tiles into `extra` pieces more (0: none), and the pieces of
+// all sequences. work: the sequences' sum of rows * keys, row_tiles that of rows, call_tiles the row tiles
+// that the call's rows make without a sequence's end; total_of(range): the sequences' sum of pieces_of.
+// Half a piece a row tile is lost by rounding up, of as many as the call's rows make: the first range
+// leaves room for that. Fewer row tiles than `extra` are then given wider ranges until there are at most
+// `extra` pieces; more of them never are, and keep the range.
+// There are at least row_tiles pieces and, with rows * (keys + range - 1) / range added up, at most
+// row_tiles + work / range <= row_tiles + extra.
+struct PieceRange {
+  int range;
+  int64_t total;
+};
+template <class Total>
+POT_BOTH PieceRange piece_range(int extra, int64_t call_tiles, int64_t work, int64_t row_tiles,
+                                Total total_of) {
+  int64_t range = kNoSplit;
+  if (extra > 0) {
+    const int64_t most = extra - (call_tiles < extra ? call_tiles : extra) / 2;
+    const int64_t even = (work + most - 1) / most;
+    range = even < kManyRange ? kManyRange : even < kNoSplit ? even : kNoSplit;
+  }
+  int64_t total = total_of((int)range);
+  for (int tries = 0; row_tiles < extra && total > extra && tries < 5; ++tries) {
+    const int64_t wider = range * (total - extra) / extra;
+    range += wider < 1 ? 1 : wider;
+    if (range > kNoSplit) range = kNoSplit;
+    total = total_of((int)range);
+  }
+  return {(int)range, total};
+}
+
 }  // namespace potattn

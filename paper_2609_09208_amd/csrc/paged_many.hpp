@@ -44,17 +44,16 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {  // sums up to and w
 
 // A workgroup's piece: row tile `tile` of sequence b, key range `split` of `splits`. A row tile's
 // keys are split when the row tiles do not fill the chip (many_extra > 0): into ranges of equal
-// length for all sequences, the shortest (to the step) for which kManyPieces of them take the whole
-// work; a short sequence's rows stay whole. However the lengths fall, there are at most one piece a
-// row tile and many_extra more. Pieces count from the last sequence's last: a prompt's late tiles, which
-// see the most keys, come first. A row tile's pieces are first .. first + splits - 1. b < 0: there is
-// no piece i. Every thread of the workgroup takes part, a sequence a thread.
+// length for all sequences (piece_range), the shortest (to the step) for which kManyPieces of them take
+// the whole work; a short sequence's rows stay whole. Pieces count from the last sequence's last: a
+// prompt's late tiles, which see the most keys, come first. A row tile's pieces are first .. first +
+// splits - 1. b < 0: there is no piece i. Every thread of the workgroup takes part, a sequence a thread.
 struct RowPiece {
   int b, tile, split, splits, first;
 };
 template <int NW>
 struct FindScratch {
-  int64_t sums[NW];
+  int64_t sums[2][NW];
   RowPiece found;
 };
 template <int NW>
@@ -62,51 +61,56 @@ __device__ __forceinline__ RowPiece find_piece(const PagedAttendArgs& a, int i, 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const ManyShape mine = many_shape(a, tid, R);
   auto shape = [&](int b0) { return b0 == 0 ? mine : many_shape(a, b0 + tid, R); };
-  auto over_group = [&](int64_t v) {
+  auto over_group = [&](auto& v) {  // each of the thread's numbers summed over the workgroup
+    constexpr int N = sizeof(v) / sizeof(v[0]);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor((long long)v, o, 64);
-    if (lane == 0) sh.sums[wave] = v;
-    __syncthreads();
-    v = 0;
+    for (int i = 0; i < N; ++i) {
 #pragma unroll
-    for (int w = 0; w < NW; ++w) v += sh.sums[w];
+      for (int o = 1; o < 64; o <<= 1) v[i] += __shfl_xor((long long)v[i], o, 64);
+      if (lane == 0) sh.sums[i][wave] = v[i];
+    }
     __syncthreads();
-    return v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) v[i] += sh.sums[i][w];
+    }
+    __syncthreads();
   };
   const int extra = a.plan.many_extra;
-  int range = 1 << 24;  // tiles
+  int64_t all[2] = {0, 0};  // work, row tiles
   if (extra > 0) {
-    int64_t work = 0;
     for (int b0 = 0; b0 < a.packed.B; b0 += 64 * NW) {
       const ManyShape m = shape(b0);
-      work += (int64_t)m.rows * m.keys;
+      all[0] += (int64_t)m.rows * m.keys;
+      all[1] += m.rows;
     }
-    // half a piece a row tile is lost by rounding up, of as many as the call's rows make
-    const int64_t most = extra - min((int64_t)extra, (int64_t)a.packed.n * a.G / R) / 2;
-    range = (int)min((int64_t)range, max((int64_t)kManyRange, (over_group(work) + most - 1) / most));
+    over_group(all);
   }
-  auto pieces = [&](const ManyShape& m) { return m.rows * ((m.keys + range - 1) / range); };
-  int64_t total = 0;
-  for (int tries = 0;; ++tries) {
-    int64_t n = 0;
-    for (int b0 = 0; b0 < a.packed.B; b0 += 64 * NW) n += pieces(shape(b0));
-    total = over_group(n);
-    if (extra == 0 || total <= extra || tries == 5) break;
-    range += max(1, (int)(range * (total - extra) / extra));
-  }
+  const PieceRange plan = piece_range(extra, (int64_t)a.packed.n * a.G / R, all[0], all[1], [&](int range) {
+    int64_t n[1] = {0};
+    for (int b0 = 0; b0 < a.packed.B; b0 += 64 * NW) {
+      const ManyShape m = shape(b0);
+      n[0] += pieces_of(m.rows, m.keys, range);
+    }
+    over_group(n);
+    return n[0];
+  });
+  const int64_t total = plan.total;
   if (tid == 0) sh.found.b = -1;
   const int64_t at = total - 1 - i;
   int64_t before = 0;  // pieces of the sequences before
   for (int b0 = 0; b0 < a.packed.B && at >= before; b0 += 64 * NW) {  // uniform
     const ManyShape m = shape(b0);
-    const int n = pieces(m), sum = wave_scan(n, lane);
-    if (lane == 63) sh.sums[wave] = sum;
+    const int n = pieces_of(m.rows, m.keys, plan.range), sum = wave_scan(n, lane);
+    if (lane == 63) sh.sums[0][wave] = sum;
     __syncthreads();
     int64_t start = before + sum - n;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      start += w < wave ? sh.sums[w] : 0;
-      before += sh.sums[w];
+      start += w < wave ? sh.sums[0][w] : 0;
+      before += sh.sums[0][w];
     }
     if (at >= start && at < start + n) {
       const int S = n / m.rows, j = (int)(at - start), tile = j / S;

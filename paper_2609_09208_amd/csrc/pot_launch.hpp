@@ -238,8 +238,8 @@ struct PagedPlan {
   int32_t few_limit, few_splits, many_rows, many_extra;
   int64_t many_tiles;  // an upper bound
 };
-// Key ranges of many rows: pieces that take the whole work together, and the shortest, in tiles.
-constexpr int kManyPieces = 512, kManyRange = 8;
+// Key ranges of many rows: pieces that take the whole work together.
+constexpr int kManyPieces = 512;
 // Floats of one row's partial: 64 sums, the reference, the weights' sum and the score factor.
 constexpr int kPartial = 68;
 
