@@ -42,7 +42,7 @@ POT_BOTH constexpr NewTokens new_tokens(int cu, int cu_next, int len, int n_rows
 // The keys that tokens p_first .. p_last of a sequence of len keys see, as 64-key tiles in
 // two runs: the sinks' (from key 0) and the window's (from key `low`, a multiple of 64). A
 // token at place p sees key j if j <= p and (j > p - window or j < n_sink); window <= 0:
-// every j <= p.
+// every j <= p. Places may lie past the keys, and then so may the window.
 struct SeenTiles {
   int sink_tiles;  // tiles 0 .. sink_tiles - 1 start at key 64 i
   int low;         // tile sink_tiles + i starts at key low + 64 i
@@ -62,7 +62,9 @@ POT_BOTH constexpr SeenTiles seen_tiles(int p_first, int p_last, int len, int wi
       sinks = 0;
     }
   }
-  return {sinks, low, sinks + (end - low + kWTile - 1) / kWTile, end};
+  const int all = (end + kWTile - 1) / kWTile;  // tiles with keys
+  if (sinks > all) sinks = all;
+  return {sinks, low, sinks + (end > low ? all - low / kWTile : 0), end};
 }
 POT_BOTH constexpr int tile_start(const SeenTiles& s, int j) {
   return j < s.sink_tiles ? j * kWTile : s.low + (j - s.sink_tiles) * kWTile;
@@ -74,6 +76,11 @@ POT_BOTH constexpr bool sees(int p, int key, int window, int n_sink) {
 POT_BOTH constexpr bool all_seen(int p_first, int p_last, int t0, int window, int n_sink) {
   return t0 + kWTile - 1 <= p_first &&
          (window <= 0 || t0 > p_last - window || t0 + kWTile <= n_sink);
+}
+// The same where the keys may end before p_first.
+POT_BOTH constexpr bool whole_tile(const SeenTiles& seen, int p_first, int p_last, int t0, int window,
+                                   int n_sink) {
+  return all_seen(p_first < seen.end ? p_first : seen.end - 1, p_last, t0, window, n_sink);
 }
 // Whether no token of them sees any.
 POT_BOTH constexpr bool none_seen(int p_first, int p_last, int t0, int window, int n_sink) {

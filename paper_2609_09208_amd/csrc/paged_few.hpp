@@ -285,7 +285,7 @@ void paged_few_kernel(const PagedAttendArgs a) {
     j += NW;
   };
   auto whole = [&](int t0, int rows8) {
-    return all_seen(p_first, p_last, t0, a.window, a.n_sink) && (UNI ? rows8 >= 0 : __all(rows8 >= 0));
+    return whole_tile(seen, p_first, p_last, t0, a.window, a.n_sink) && (UNI ? rows8 >= 0 : __all(rows8 >= 0));
   };
 #pragma nounroll
   while (j < run.end) {

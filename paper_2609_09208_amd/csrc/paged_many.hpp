@@ -209,7 +209,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
     }
   };
   auto stage = [&](int t0, int buf) {
-    const bool part = !all_seen(wg_first, wg_last, t0, a.window, a.n_sink);
+    const bool part = !whole_tile(seen, wg_first, wg_last, t0, a.window, a.n_sink);
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
       const int g = wave + NW * i, key = 8 * g + (lane >> 3), d = lane & 7;
@@ -362,7 +362,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
     const int4 f0 = *reinterpret_cast<const int4*>(&flags[buf][0]);
     const int4 f1 = *reinterpret_cast<const int4*>(&flags[buf][4]);
     const int any = __builtin_amdgcn_readfirstlane(f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w);
-    compute(!all_seen(w_first, w_last, t0, a.window, a.n_sink) || (any & 1), t0, buf);
+    compute(!whole_tile(seen, w_first, w_last, t0, a.window, a.n_sink) || (any & 1), t0, buf);
     special |= (any & 2) != 0;
   };
 
@@ -386,7 +386,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
 #pragma nounroll
     for (int j = run.first; j < run.end; ++j) {
       const int t0 = tile_start(seen, j);
-      if (all_seen(wg_first, wg_last, t0, a.window, a.n_sink)) continue;
+      if (whole_tile(seen, wg_first, wg_last, t0, a.window, a.n_sink)) continue;
       const SeenKeys sk = seen_keys(a, place, seen.end, t0 + 8 * half);
 #pragma nounroll
       for (int b = 0; b < 4; ++b) {
