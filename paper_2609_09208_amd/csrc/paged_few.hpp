@@ -238,6 +238,7 @@ void paged_few_kernel(const PagedAttendArgs a) {
     }
     const float shift = weight_shift(ref);
     uint32_t hi[kHalves][4], lo[kHalves][4];
+    float tile_l = 0.0f;  // the tile's weights go onto l together: each alone would be rounded at l's size
 #pragma unroll
     for (int kb = 0; kb < kHalves; ++kb)
 #pragma unroll
@@ -245,14 +246,15 @@ void paged_few_kernel(const PagedAttendArgs a) {
         const float p0 = weight_of(y[kb][2 * i], c, shift), p1 = weight_of(y[kb][2 * i + 1], c, shift);
         hi[kb][i] = pack_half(p0, p1);
         if constexpr (LOW) {
-          l += p0;
-          l += p1;
+          tile_l += p0;
+          tile_l += p1;
         } else {  // of the weights as they are multiplied
           const half2v ones = {(_Float16)1.0f, (_Float16)1.0f};
-          l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[kb][i]), ones, l, false);
+          tile_l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[kb][i]), ones, tile_l, false);
         }
         if constexpr (LOW) lo[kb][i] = low_part(p0, p1, hi[kb][i]);
       }
+    l += tile_l;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const int at = EIGHT ? 0 : kb;  // of the weights

@@ -328,6 +328,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
       s[1] -= ref.m;
     }
     const float shift = weight_shift(ref);
+    float tile_l = 0.0f;  // the tile's weights go onto l together: each alone would be rounded at l's size
 #pragma unroll
     for (int b = 0; b < 4; ++b) {  // 16 keys at a time
       const int kb = b >> 1, e0 = 8 * (b & 1);
@@ -337,11 +338,11 @@ void paged_many_kernel(const PagedAttendArgs a) {
         const float p0 = weight_of(s[kb][e0 + 2 * i], c, shift), p1 = weight_of(s[kb][e0 + 2 * i + 1], c, shift);
         hi[i] = pack_half(p0, p1);
         if constexpr (LOW) {
-          l += p0;
-          l += p1;
+          tile_l += p0;
+          tile_l += p1;
           lo[i] = low_part(p0, p1, hi[i]);
         } else {  // of the weights as they are multiplied
-          l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[i]), kOnes, l, false);
+          tile_l = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, hi[i]), kOnes, tile_l, false);
         }
       }
 #pragma unroll
@@ -355,6 +356,7 @@ void paged_many_kernel(const PagedAttendArgs a) {
         }
       }
     }
+    l += tile_l;
   };
   bool special = false;  // a tile in part held special values (paged.hpp); uniform
   auto tile = [&](int t0, int buf) {
