@@ -573,12 +573,14 @@ pot_status check_pages(const pot_format* fmt, const pot_pages* p, const int32_t*
   if (n > (1 << 23)) return fail(POT_ERR_UNSUPPORTED, "n %d > 2^23", n);
   if ((fmt->mant_bits > 0) != (p->codes_m != nullptr))
     return fail(POT_ERR_INVALID_ARG, "codes_m must be non-NULL exactly when mant_bits > 0");
-  if (!p->codes_se || !p->key_scale || !p->values || !p->table)
+  // without sequences the table and the lengths have no elements, and no address
+  if (!p->codes_se || !p->key_scale || !p->values || (B > 0 && !p->table))
     return fail(POT_ERR_INVALID_ARG, "codes_se, key_scale, values or table is NULL");
   if (!aligned(p->codes_se, 16) || !aligned(p->codes_m, 8) || !aligned(p->key_scale, 16) ||
       !aligned(p->values, 16) || !aligned(p->table, 4))
     return fail(POT_ERR_INVALID_ARG, "misaligned codes_se / codes_m / key_scale / values / table");
-  if (!cu_new || !seq_lens) return fail(POT_ERR_INVALID_ARG, "cu_new or seq_lens is NULL");
+  if (B > 0 && (!cu_new || !seq_lens))
+    return fail(POT_ERR_INVALID_ARG, "cu_new or seq_lens is NULL");
   if (!aligned(cu_new, 4) || !aligned(seq_lens, 4))
     return fail(POT_ERR_INVALID_ARG, "cu_new and seq_lens must be 4-byte aligned");
   const uint32_t groups = (uint32_t)p->page_size / 8;
