@@ -642,6 +642,9 @@ def pot_paged_attention(fmt: pot_format, q, pages: pot_pages, cu_new, seq_lens, 
     if workspace is None:
         ws = ws_bytes = 0
     else:
+        if not isinstance(workspace, int) and (workspace.get_device() != device
+                                               or not workspace.is_contiguous()):
+            _mismatch("a dense workspace on the queries' GPU is needed")
         ws = _ptr(workspace)
         if ws_bytes is None:
             ws_bytes = workspace.numel() * workspace.element_size()
