@@ -87,6 +87,22 @@ POT_BOTH constexpr bool none_seen(int p_first, int p_last, int t0, int window, i
   return t0 > p_last || (window > 0 && t0 + kWTile - 1 <= p_first - window && t0 >= n_sink);
 }
 
+// Which of a tile's keys a query at `place` sees, t0 the tile's first, keys at or past `end` not there:
+// key t0 + e is seen if e <= last and (e > before or e < sinks).
+struct SeenKeys {
+  int last, before, sinks;
+};
+POT_BOTH constexpr SeenKeys seen_keys(int place, int end, int t0, int window, int n_sink) {
+  return {(place < end - 1 ? place : end - 1) - t0, window > 0 ? place - window - t0 : -1, n_sink - t0};
+}
+// The keys t0 + e0 .. t0 + e0 + 7 that it sees as bits.
+POT_BOTH constexpr uint32_t first_bits(int n) {  // of 8
+  return (1u << (n < 0 ? 0 : n > 8 ? 8 : n)) - 1u;
+}
+POT_BOTH constexpr uint32_t seen_bits(const SeenKeys& s, int e0) {
+  return first_bits(s.last + 1 - e0) & (~first_bits(s.before + 1 - e0) | first_bits(s.sinks - e0)) & 0xFFu;
+}
+
 // Tiles j0 .. j1 - 1 of split i of n.
 struct TileRun {
   int first, end;

@@ -19,11 +19,6 @@ __device__ __forceinline__ uint4 stream16(const void* p) {
   const u32x4v v = __builtin_nontemporal_load(static_cast<const u32x4v*>(p));
   return make_uint4(v.x, v.y, v.z, v.w);
 }
-typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint2 stream8(const void* p) {
-  const u32x2v v = __builtin_nontemporal_load(static_cast<const u32x2v*>(p));
-  return make_uint2(v.x, v.y);
-}
 
 // A group's rows of the pool are counted by groups: row8 = row / 8, below 2^31.
 // First cache row / 8 of group `group` of a sequence for a kv head: group `in` of its page;
@@ -166,21 +161,8 @@ __device__ __forceinline__ uint4 mask_tokens(uint4 v, int first, int end) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Which of a tile's keys a query sees, t0 the tile's first: key t0 + e is seen if e <= last and
-// (e > before or e < sinks).
-struct SeenKeys {
-  int last, before, sinks;
-};
 __device__ __forceinline__ SeenKeys seen_keys(const PagedAttendArgs& a, int place, int end, int t0) {
-  return {min(place, end - 1) - t0, a.window > 0 ? place - a.window - t0 : -1, a.n_sink - t0};
-}
-__device__ __forceinline__ bool is_seen(const SeenKeys& s, int e) {
-  return e <= s.last && (e > s.before || e < s.sinks);
-}
-// The same of keys e0 .. e0 + 7 as bits.
-__device__ __forceinline__ uint32_t seen_bits(const SeenKeys& s, int e0) {
-  auto below = [](int n) { return (1u << min(max(n, 0), 8)) - 1u; };  // keys of the 8 before the n-th
-  return below(s.last + 1 - e0) & (~below(s.before + 1 - e0) | below(s.sinks - e0)) & 0xFFu;
+  return seen_keys(place, end, t0, a.window, a.n_sink);
 }
 // y where bit e of the mask is set, minus infinity elsewhere.
 __device__ __forceinline__ float if_seen(float y, uint32_t mask, int e) {
@@ -241,11 +223,6 @@ __device__ __forceinline__ void store_out4(void* out, int64_t at, int type, floa
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
   else
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack_half(a, b), pack_half(c, d));
-}
-__device__ __forceinline__ void store_out1(void* out, int64_t at, int type, float a) {
-  if (type == POT_FP32) static_cast<float*>(out)[at] = a;
-  else if (type == POT_BF16) static_cast<uint16_t*>(out)[at] = (uint16_t)pack_bf16(a, a);
-  else static_cast<uint16_t*>(out)[at] = (uint16_t)pack_half(a, a);
 }
 
 // A query's reference m (a sum times its scale), and b = 7 - m c as rounded: a key's weight is
