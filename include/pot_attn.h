@@ -358,7 +358,7 @@ typedef struct pot_pages {
  *               is negative is stored nowhere.
  *  n            rows, up to 2^23. B up to 65535.
  * Two tokens that come to the same cache row leave one of them or a mixture. Outputs alias
- * nothing. B or n of 0 is a no-op. */
+ * nothing. B or n of 0 is a no-op; with B of 0 table, cu_new and seq_lens may be NULL. */
 pot_status pot_paged_append(const pot_format* fmt, const pot_rope* rope, int32_t dtype,
                             const pot_part* parts, int32_t weight_dtype, float eps,
                             const int64_t* positions, const double* inv_freq,
@@ -399,8 +399,8 @@ size_t pot_paged_workspace_bytes(int32_t B, int32_t n, int32_t Hq, int32_t Hkv, 
  *  out          dense [n][Hq][64], device, 16-byte aligned; may not alias q or the cache.
  *  workspace    >= pot_paged_workspace_bytes(...) bytes, 256-byte aligned; any contents. Calls that
  *               share one must not overlap in time.
- * Results do not differ from call to call. B or n of 0 is a no-op. n up to 2^23, B up to 65535, and
- * n * Hq / 256 + B * Hkv below 2^23 - 512. */
+ * Results do not differ from call to call. B or n of 0 is a no-op (as pot_paged_append). n up to 2^23,
+ * B up to 65535, and n * Hq / 256 + B * Hkv below 2^23 - 512. */
 pot_status pot_paged_attention(const pot_format* fmt, int32_t dtype, const void* q,
                                int64_t stride_t, int64_t stride_h, const pot_pages* pages,
                                const int32_t* cu_new, const int32_t* seq_lens,

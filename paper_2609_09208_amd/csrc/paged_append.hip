@@ -6,8 +6,9 @@
 // Bound: the stream of many tokens (rows in, queries out: 9/10 of the bytes at 32 + 4 + 4 heads);
 // of few a chain of round trips: the sequence's bounds, its length and page, the row. Measured (32 + 4 + 4
 // heads): 1 token 5 us, 64 sequences of one 6, 8192 tokens bf16 to k = 4 and fp16 values 19.5 (97 MB with what
-// reads them back: 4 TB/s); 2300 tokens of fp32 with rotated keys, k = 2, 16 + 8 + 8 heads, 15.5 (VALU: the
-// encoder's divisions and both rotations).
+// reads them back: 4 TB/s; VALU busy for 60% of the time that the CUs are); 2300 tokens of fp32 with rotated
+// keys, k = 2, 16 + 8 + 8 heads, 15.5 (VALU 51%, the encoder's divisions and both rotations most of it, in few
+// waves that wait for the same chain).
 #include "encode_rows.hpp"
 #include "head_rows.hpp"
 #include "paged.hpp"

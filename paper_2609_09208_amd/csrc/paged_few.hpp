@@ -13,7 +13,7 @@
 // sequence's end, the window's, pages that are not there) go through the same code with them.
 //
 // Bound: the stream with fp16 values (164 bytes a key: 64 x 8192 keys 63 us, 5.5 TB/s; with a window
-// of 4096 33, 30 in one range); with 4-bit values (72 bytes) VALU issue, 65 - 70% busy of 343
+// of 4096 33, 30 in one range); with 4-bit values (72 bytes) VALU issue, 71 - 74% busy of 345
 // operations a tile, most of them the operands' (64 x 16384 keys 62 us, 4.9 TB/s; 64 x 8192 34). Pages
 // cost nothing: pages of 128 and of 32768 keys differ by 1%.
 #pragma once

@@ -9,12 +9,15 @@
 // query's reference, sum and outputs are its two lanes' own. The reference rises only when weights
 // would leave fp16's range.
 //
-// Bound: VALU issue. Of 32 rows and 64 keys a wave has 16 matrix instructions and 215 operations (at k = 1
-// and fp16 values; 330 at k = 4 and 4 bits): two products, an exponential and its half of a maximum, of a
-// pack and of a sum a score, then the tile's staging. VALU is 74% busy, the matrix cores 32%; four waves a
-// SIMD, for which the queries stand in LDS (one row block a wave at 128 registers; two blocks at 256 took 430
-// us where this takes 410, two blocks whose weights and products alternate 560, 16 waves a workgroup 399 but
-// more on short calls). 8192 tokens of 32 + 4 heads, k = 1, fp16 values: 410 us, 670 TFLOP/s.
+// Bound: VALU issue. Of 32 rows and 64 keys a wave has 16 matrix instructions and 216 operations (at k = 1
+// and fp16 values; 331 at k = 4 and 4 bits): two products, an exponential and its half of a maximum, of a
+// pack and of a sum a score, then the tile's staging. Counted over whole calls, with the tiles at the
+// diagonal and the window's ends, 16.8 VALU instructions a matrix instruction, itself among them, and 28.2.
+// VALU is 74% busy in both, the matrix cores 32% and 19%; four waves a SIMD, for which the queries stand in
+// LDS (one row block a wave at 128 registers; when this took 410 us, two blocks at 256 took 430, two blocks
+// whose weights and products alternate 560, 16 waves a workgroup 399 but more on short calls). 8192 tokens of
+// 32 + 4 heads, k = 1, fp16 values: 417 us, 660 TFLOP/s; 2 x 2048 tokens with a window of 1000, k = 4, 4 bits:
+// 81 us.
 #pragma once
 
 #include "paged.hpp"
@@ -145,7 +148,11 @@ __device__ __forceinline__ uint4 quad_dwords(uint32_t x) {
 }
 
 
-// R: rows of a tile. LOW: the weights' rounding goes into the products too (outputs of 32 bits).
+// R: rows of a tile. LOW: what rounding to fp16 leaves of the weights goes into the products too. Outputs of
+// 32 bits have it. For outputs of 16 bits that rounding (half a step of fp16) is no larger than the output's
+// own: their error against 64 bits is 1.7e-3 of the outputs' size for bf16, as with weights of 32 bits, and
+// 2.5e-4 for fp16 (2.1e-4 with weights of 32 bits); LOW takes 8192 tokens from 417 us to 536 and 512 on 8192
+// keys from 74 to 87.
 template <int K, int VF, int R, bool LOW>
 __global__ __launch_bounds__(2 * R) __attribute__((amdgpu_waves_per_eu(R == 128 ? 3 : 4)))
 void paged_many_kernel(const PagedAttendArgs a) {
@@ -271,8 +278,8 @@ void paged_many_kernel(const PagedAttendArgs a) {
   const half2v kOnes = {(_Float16)1.0f, (_Float16)1.0f};
   auto compute = [&](bool part, int t0, int buf) {
     // Places in LDS. Where a tile's loads take the most registers they are made anew for each tile: kept
-    // through the loop, they leave reloads from memory behind the loads under way (2048 tokens with a window of
-    // 1000, k = 4, 4 bits: 81 us against 84; at k = 1 and fp16 values 432 against 426).
+    // through the loop, they leave reloads from memory behind the loads under way (2 x 2048 tokens with a window
+    // of 1000, k = 4, 4 bits: 82 us, kept 85; 8192 tokens, k = 1, fp16 values: 438, kept 431).
     int ln = lane;
     if constexpr (K > 0 && VF == POT_VALUES_INT4) asm volatile("" : "+v"(ln));
     const int col = ln & 31, half = ln >> 5;
